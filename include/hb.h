@@ -473,6 +473,106 @@ HB_API int hb_pool_chunk_noalloc(const float* x, const void* gain, int32_t n_row
                                  float rms_eps, int32_t mode, int32_t first_chunk, int32_t is_final,
                                  float* slot_sum, uint32_t* slot_meta, float* out_emb, void* stream);
 
+/* ---- 8-bit KV cache ---------------------------------------------------------
+ *
+ * The paged KV cache with one byte per element (e4m3: 4 exponent and 3 mantissa bits) and a scale
+ * for each block of one page (16 tokens) and KV head, K and V apart: half the memory and half the
+ * bytes a decode row has to read.  Arena layout: [layer][page][kv head][block], block =
+ *   16 * head_dim codes of K: token t, dimension d at byte (d / 64) * 1024 + t * 64 + d % 64
+ *   16 * head_dim codes of V: token t, dimension d at byte
+ *       (d / 32) * 512 + (d % 8 * 4 + t % 8 / 2) * 16 + d % 32 / 8 * 4 + t / 8 * 2 + t % 2
+ *   32 bytes: float scale of K, float scale of V (powers of two), 24 bytes reserved
+ * (a block is read with ONE bulk copy and its 16-byte pieces are the matrix-instruction fragments).
+ * A code c stands for c * scale.  The scale is the smallest 2^e, -32 <= e <= 24, with
+ * max |x| <= 448 * 2^e over the rows appended to the block (448 is the largest e4m3 value).  A power
+ * of two, because then neither the codes nor the products with them are rounded by it, and a code
+ * that has to be stored again under a larger scale only changes where it falls below the smallest
+ * normal e4m3 value.  An append that starts at slot 0 of a page starts the block afresh (its
+ * unused slots become zero); one that starts later keeps the larger of the block's scale and its own,
+ * and stores the block's codes again if the scale grew.  Infinite elements saturate, NaN stays NaN. */
+
+/* Bytes of an 8-bit arena of n_pages.  Host only. */
+HB_API int hb_kv8_arena_bytes(const hb_model_cfg* cfg, int32_t n_pages, size_t* out_bytes);
+/* hb_kv_create for the 8-bit format: an hb_kv whose pages are allocated, freed and destroyed with
+ * the hb_kv_* calls above, and which hb_mixed_step[_lora] takes in place of a 16-bit cache (the
+ * step's QKV projection then leaves fp16 rows for hb_kv8_append, and hb_kv8_attention reads the
+ * pages).  Arena 256-byte aligned. */
+HB_API int hb_kv8_create(const hb_model_cfg* cfg, void* arena, size_t arena_bytes, int32_t n_pages, hb_kv** out);
+
+/* The rows of a step, in DEVICE memory the caller owns.  Of each segment q_start, q_len, pos_start,
+ * pt_start and pt_len are read (the other fields are not).  Unlike in hb_batch_desc, segments need
+ * not be adjacent and q_len may be 0; rows whose row_seg is -1 belong to nobody (padding): what
+ * the calls write for rows is left untouched there.  Nothing is read on the host, so a captured
+ * call sees what the arrays hold when it is replayed.  The two bounds size the launches: a segment
+ * beyond one of them, a page id outside the arena, or any other inconsistent field is reported
+ * through the status word (HB_STATUS_APPEND_INDEX / HB_STATUS_ATTN_INDEX) and skipped. */
+typedef struct {
+  const hb_seg* segs;        /* device [n_segs], 16-byte aligned                        */
+  const int32_t* page_ids;   /* device [n_page_ids]                                     */
+  const int32_t* row_seg;    /* device [n_rows]: the row's segment, -1 = padding        */
+  int32_t n_segs, n_page_ids, n_rows;
+  int32_t max_q_len;         /* no segment has more rows                                */
+  int32_t max_keys;          /* no segment has a larger pos_start + q_len               */
+} hb_rows;
+
+/* Which pairs of a head's first rot_dim dimensions turn together: (2i, 2i + 1), or (i, i + rot_dim / 2). */
+enum { HB_ROPE_PAIRS = 0, HB_ROPE_HALVES = 1 };
+
+/* What hb_kv8_append reads and writes besides the cache.  Device pointers.
+ *   qkv       fp16 [n_rows, qkv_stride]: per row n_heads q heads, n_kv_heads k heads, n_kv_heads v
+ *             heads of head_dim; 16-byte aligned, stride a multiple of 8
+ *   q_out     fp16 [n_rows, q_stride]: the row's normed and rotated q heads; may be the q part of qkv
+ *   q_gain, k_gain  bf16 [head_dim] (16-byte aligned) or NULL: x <- x / sqrt(mean(x^2) + norm_eps) * gain per head
+ *   rope_cos, rope_sin  fp32 [rope_rows, rot_dim / 2] (16-byte aligned), row = position; rot_dim a
+ *             multiple of 16 up to head_dim, 0 = no rotation (the tables are not read)
+ * Norm, rotation and scaling run in fp32; q is rounded once to fp16 (saturating), k once to e4m3. */
+typedef struct {
+  const void* qkv;
+  void* q_out;
+  int64_t qkv_stride, q_stride;   /* elements */
+  const void *q_gain, *k_gain;
+  float norm_eps;
+  const float *rope_cos, *rope_sin;
+  int32_t rope_rows, rot_dim, rope_layout;
+} hb_append_args;
+
+/* Norms, rotates and appends the k and v of every row to layer `layer` of an 8-bit cache at position
+ * pos_start + (row - q_start), and writes the rotated q.  A page written by one segment must not be
+ * written by another of the same call.  ctx supplies the status word (same cfg as the cache's). */
+HB_API int hb_kv8_append(hb_ctx* ctx, hb_kv* kv, int32_t layer, const hb_rows* rows, const hb_append_args* args, void* stream);
+
+/* Causal attention of every row over its own request's pages of an 8-bit cache (the rows' own k and
+ * v included: append first): row j of a segment sees positions 0 .. pos_start + j.
+ *   q    fp16 [n_rows, q_stride], out fp16 [n_rows, out_stride]: n_heads heads of head_dim; 16-byte
+ *        aligned, strides multiples of 8; out may not overlap q
+ *   scale  factor of the scores (0 = 1 / sqrt(head_dim))
+ *   workspace  device, 256-byte aligned, hb_kv8_attention_workspace bytes for these rows; needs no
+ *        initialisation and belongs to the call until it has run: calls that may run at the same
+ *        time need a workspace each
+ * Scores, softmax and sums in fp32, probabilities rounded to fp16 for the tensor cores.  How a
+ * segment's keys are split depends on its own lengths only, never on the rest of the batch. */
+HB_API int hb_kv8_attention_workspace(const hb_model_cfg* cfg, const hb_rows* rows, size_t* out_bytes);
+HB_API int hb_kv8_attention(hb_ctx* ctx, hb_kv* kv, int32_t layer, const hb_rows* rows, const void* q, int64_t q_stride,
+                     void* out, int64_t out_stride, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rotary tables for hb_kv8_append: out_cos / out_sin HOST float [n_pos, rot_dim / 2], angle(p, i) =
+ * p * f_i with f_i = theta^(-2i / rot_dim), formed in double and stored as float.  Scaling for
+ * contexts longer than the trained one (NULL = none):
+ *   HB_ROPE_LINEAR  f_i / factor for every i
+ *   HB_ROPE_BY_PARTS  with r_i = orig_len * f_i / (2 pi) turns over the trained length:
+ *       g_i = clamp((r_i - lo) / (hi - lo), 0, 1);  f_i * (g_i + (1 - g_i) / factor)
+ *       (fast dimensions stay, slow ones are interpolated; Peng et al. 2023, "YaRN", section 3.2)
+ *   both: cos and sin are multiplied by `attn_factor` (1 = unchanged)
+ * Host only. */
+enum { HB_ROPE_LINEAR = 1, HB_ROPE_BY_PARTS = 2 };
+typedef struct {
+  int32_t kind;
+  double factor;        /* >= 1 */
+  double orig_len, lo, hi;   /* BY_PARTS: orig_len > 0, 0 <= lo < hi */
+  double attn_factor;   /* > 0 */
+} hb_rope_scaling;
+HB_API int hb_rope_table(int32_t n_pos, int32_t rot_dim, double theta, const hb_rope_scaling* scaling, float* out_cos, float* out_sin);
+
 #ifdef __cplusplus
 }
 #endif

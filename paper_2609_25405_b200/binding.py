@@ -18,7 +18,8 @@ ERRORS = {0: "HB_OK", -1: "HB_ERR_BAD_ARG", -2: "HB_ERR_CUDA", -3: "HB_ERR_OOM_P
           -4: "HB_ERR_OOM_SLOTS", -5: "HB_ERR_TOO_LARGE", -6: "HB_ERR_BAD_DESC",
           -7: "HB_ERR_DEVICE_STATUS", -8: "HB_ERR_UNSUPPORTED"}
 from .consts import (KIND_DECODE, KIND_PREFILL_CHUNK, KIND_EMBED_CHUNK, POOL_NONE, POOL_MEAN,  # noqa: F401,E402
-                     POOL_LAST, POOL_CLS, POOL_WMEAN, POOL_MAX, EPI_F16, EPI_F32, EPI_RESID_F32, EPI_SWIGLU, CLASSES)
+                     POOL_LAST, POOL_CLS, POOL_WMEAN, POOL_MAX, EPI_F16, EPI_F32, EPI_RESID_F32, EPI_SWIGLU, CLASSES,
+                     ROPE_PAIRS, ROPE_HALVES, ROPE_LINEAR, ROPE_BY_PARTS)
 
 
 class HbError(RuntimeError):
@@ -64,6 +65,22 @@ class BatchDesc(C.Structure):
                 ("page_ids", C.POINTER(C.c_int32))]
 
 
+class RowsStruct(C.Structure):
+    _fields_ = [("segs", C.c_void_p), ("page_ids", C.c_void_p), ("row_seg", C.c_void_p), ("n_segs", C.c_int32),
+                ("n_page_ids", C.c_int32), ("n_rows", C.c_int32), ("max_q_len", C.c_int32), ("max_keys", C.c_int32)]
+
+
+class AppendArgs(C.Structure):
+    _fields_ = [("qkv", C.c_void_p), ("q_out", C.c_void_p), ("qkv_stride", C.c_int64), ("q_stride", C.c_int64),
+                ("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("norm_eps", C.c_float), ("rope_cos", C.c_void_p),
+                ("rope_sin", C.c_void_p), ("rope_rows", C.c_int32), ("rot_dim", C.c_int32), ("rope_layout", C.c_int32)]
+
+
+class RopeScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("factor", C.c_double), ("orig_len", C.c_double), ("lo", C.c_double),
+                ("hi", C.c_double), ("attn_factor", C.c_double)]
+
+
 SEG_DTYPE = np.dtype([(n, np.int32) for n, _ in Seg._fields_])
 
 if not os.path.exists(LIB_PATH):
@@ -82,6 +99,13 @@ _sig = {
     "hb_kv_alloc_pages": [_P, C.c_int32, C.POINTER(C.c_int32)],
     "hb_kv_free_pages": [_P, C.c_int32, C.POINTER(C.c_int32)],
     "hb_kv_free_count": [_P, C.POINTER(C.c_int32)],
+    "hb_kv8_arena_bytes": [C.POINTER(ModelCfg), C.c_int32, C.POINTER(C.c_size_t)],
+    "hb_kv8_create": [C.POINTER(ModelCfg), _P, C.c_size_t, C.c_int32, C.POINTER(_P)],
+    "hb_kv8_append": [_P, _P, C.c_int32, C.POINTER(RowsStruct), C.POINTER(AppendArgs), _P],
+    "hb_kv8_attention_workspace": [C.POINTER(ModelCfg), C.POINTER(RowsStruct), C.POINTER(C.c_size_t)],
+    "hb_kv8_attention": [_P, _P, C.c_int32, C.POINTER(RowsStruct), _P, C.c_int64, _P, C.c_int64, C.c_float, _P,
+                         C.c_size_t, _P],
+    "hb_rope_table": [C.c_int32, C.c_int32, C.c_double, C.POINTER(RopeScaling), _P, _P],
     "hb_pool_arena_bytes": [C.POINTER(ModelCfg), C.c_int32, C.POINTER(C.c_size_t)],
     "hb_pool_create": [C.POINTER(ModelCfg), _P, C.c_size_t, C.c_int32, C.POINTER(_P)],
     "hb_pool_destroy": [_P],
@@ -406,6 +430,123 @@ class KvCache:
             pass
 
 
+def kv8_arena_bytes(cfg, n_pages):
+    nbytes = C.c_size_t()
+    check(lib.hb_kv8_arena_bytes(C.byref(cfg), n_pages, C.byref(nbytes)), "hb_kv8_arena_bytes")
+    return nbytes.value
+
+
+class KvCache8(KvCache):
+    """8-bit KV arena (e4m3 codes, one power-of-two scale per page and KV head for K and for V) + the
+    library's page free list.  `arena`: a uint8 tensor to use instead of allocating one."""
+
+    def __init__(self, cfg, n_pages, device="cuda", fill=None, arena=None):
+        self.cfg = cfg
+        self.n_pages = n_pages
+        nbytes = kv8_arena_bytes(cfg, n_pages)
+        self.handle = C.c_void_p()
+        self.arena = None
+        if device is not None:
+            if arena is not None:
+                if arena.dtype != torch.uint8 or not arena.is_contiguous() or arena.numel() < nbytes or not arena.is_cuda:
+                    raise ValueError("arena: a contiguous uint8 tensor on the GPU that holds n_pages")
+                self.arena = arena[:nbytes]
+            else:
+                self.arena = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            if fill is not None:
+                self.arena.fill_(fill)
+        ptr = C.c_void_p(self.arena.data_ptr()) if self.arena is not None else None
+        check(lib.hb_kv8_create(C.byref(cfg), ptr, nbytes, n_pages, C.byref(self.handle)), "hb_kv8_create")
+
+    def _blocks(self):
+        c = self.cfg
+        return self.arena.view(c.n_layers, self.n_pages, c.n_kv_heads, 32 * c.head_dim + 32)
+
+    def codes(self):
+        """[L, page, Hkv, 32 * Dh] float8_e4m3fn view: K codes, then V codes, in the arena's own order."""
+        return self._blocks()[..., :32 * self.cfg.head_dim].view(torch.float8_e4m3fn)
+
+    def scales(self):
+        """[L, page, Hkv, 2] fp32 view: scale of K, scale of V."""
+        d = 32 * self.cfg.head_dim
+        return self._blocks()[..., d:d + 8].view(torch.float32)
+
+    def view(self):
+        raise TypeError("an 8-bit arena has no 16-bit view: use codes() and scales(), or rows()")
+
+    def rows(self, layer, pages, slots, is_v):
+        """K (is_v = 0) or V (1) rows of `layer` at (pages[i], slots[i]) as [n, Hkv, Dh] fp32 (code * scale)."""
+        dh = self.cfg.head_dim
+        d = torch.arange(dh, device=self.arena.device)
+        t = torch.as_tensor(slots, device=self.arena.device).view(-1, 1)
+        if is_v:
+            at = 16 * dh + d // 32 * 512 + (d % 8 * 4 + t % 8 // 2) * 16 + d % 32 // 8 * 4 + t // 8 * 2 + t % 2
+        else:
+            at = d // 64 * 1024 + t * 64 + d % 64
+        pages = torch.as_tensor(pages, device=self.arena.device)
+        bytes_ = self._blocks()[layer][pages].gather(2, at[:, None].expand(-1, self.cfg.n_kv_heads, -1))
+        return bytes_.view(torch.float8_e4m3fn).float() * self.scales()[layer][pages][..., is_v, None]
+
+
+class SegRows:
+    """The rows of a step in device memory, as the operators over the 8-bit cache read them: segs int32
+    [R, 12] (SEG_DTYPE), page_ids int32, row_seg int32 [T] (segment of each row, -1 = padding).
+    max_q_len / max_keys bound every segment's q_len and pos_start + q_len."""
+
+    def __init__(self, segs, page_ids, row_seg, max_q_len, max_keys):
+        for t, n in ((segs, "segs"), (page_ids, "page_ids"), (row_seg, "row_seg")):
+            if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.device != segs.device:
+                raise ValueError(f"{n}: a contiguous int32 tensor on the GPU")
+        if segs.dim() != 2 or segs.shape[1] != 12 or page_ids.dim() != 1 or row_seg.dim() != 1:
+            raise ValueError("segs [R, 12], page_ids [n], row_seg [T]")
+        self.segs, self.page_ids, self.row_seg = segs, page_ids, row_seg
+        self.device = segs.device
+        self.struct = RowsStruct(segs.data_ptr(), page_ids.data_ptr(), row_seg.data_ptr(), segs.shape[0],
+                                 page_ids.shape[0], row_seg.shape[0], int(max_q_len), int(max_keys))
+
+    @classmethod
+    def from_batch(cls, batch, device="cuda"):
+        """Upload a Batch's segments and page lists."""
+        segs = batch.segs
+        row_seg = np.repeat(np.arange(len(segs), dtype=np.int32), segs["q_len"])
+        up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(device)
+        return cls(up(segs.view(np.int32).reshape(len(segs), 12)), up(batch.page_ids), up(row_seg),
+                   int(segs["q_len"].max(initial=0)), int((segs["pos_start"] + segs["q_len"]).max(initial=0)))
+
+
+class Rope:
+    """Rotary tables on the device: cos / sin fp32 [positions, rot_dim / 2], and which dimensions pair up."""
+
+    def __init__(self, cos, sin, layout=ROPE_PAIRS):
+        for t in (cos, sin):
+            if t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous() or t.dim() != 2 or t.shape != cos.shape:
+                raise ValueError("cos / sin: contiguous fp32 tensors [positions, rot_dim / 2] on the GPU")
+        self.cos, self.sin, self.layout = cos, sin, layout
+
+    @classmethod
+    def table(cls, n_pos, rot_dim, theta, layout=ROPE_PAIRS, scaling=None, device="cuda"):
+        """Tables from hb_rope_table; `scaling`: RopeScaling or None."""
+        cos, sin = rope_table(n_pos, rot_dim, theta, scaling)
+        return cls(torch.from_numpy(cos).to(device), torch.from_numpy(sin).to(device), layout)
+
+
+def rope_table(n_pos, rot_dim, theta, scaling=None):
+    """(cos, sin) numpy fp32 [n_pos, rot_dim / 2] (host only)."""
+    cos = np.empty((max(int(n_pos), 0), max(int(rot_dim), 0) // 2), dtype=np.float32)
+    sin = np.empty_like(cos)
+    check(lib.hb_rope_table(n_pos, rot_dim, float(theta), C.byref(scaling) if scaling is not None else None,
+                            cos.ctypes.data_as(_P), sin.ctypes.data_as(_P)), "hb_rope_table")
+    return cos, sin
+
+
+def _rows_f16(t, rows, cols, device, name):
+    """A [>= rows, cols] fp16 matrix with unit column stride: (pointer, row stride)."""
+    if t.dtype != torch.float16 or t.device != device or t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or \
+            (t.numel() and t.stride(1) != 1):
+        raise ValueError(f"{name}: an fp16 tensor [{rows}, {cols}] with unit column stride on {device}")
+    return C.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), cols))
+
+
 class Pool:
     """Caller-owned pooling arena (torch) + the library's slot free list."""
 
@@ -493,6 +634,7 @@ class Context:
             raise RuntimeError("libhb needs a CUDA device (B200); there is no CPU path")
         self.cfg = cfg
         self.handle = C.c_void_p()
+        self.device = torch.device("cuda", torch.cuda.current_device())
         check(lib.hb_create(C.byref(cfg), max_tokens, max_segs, max_page_ids, None, 0, C.byref(self.handle)),
               "hb_create")
 
@@ -525,6 +667,55 @@ class Context:
                                 C.c_void_p(slot_meta.data_ptr()),
                                 C.c_void_p(out_emb.data_ptr()) if out_emb is not None else None,
                                 _stream_ptr(stream)), "hb_pool_chunk")
+
+    def _same_device(self, rows, kv):
+        if not isinstance(kv, KvCache8):
+            raise TypeError("an 8-bit cache (KvCache8)")
+        if rows.device != self.device or kv.arena is None or kv.arena.device != self.device:
+            raise ValueError(f"rows and cache on the context's device, {self.device}")
+        return self.device
+
+    def kv8_append(self, kv, layer, rows, qkv, q_out, rope=None, q_norm=None, k_norm=None, norm_eps=1e-6, stream=None):
+        """hb_kv8_append: head norms (bf16 gains [Dh] or None), rotation (Rope or None), K / V of every row of
+        `rows` (SegRows) appended to layer `layer` of a KvCache8; qkv fp16 [T, (Hq + 2 Hkv) Dh], q_out
+        fp16 [T, Hq Dh] (rows may be strided views)."""
+        c = self.cfg
+        T, dev = rows.struct.n_rows, self._same_device(rows, kv)
+        a = AppendArgs()
+        a.qkv, a.qkv_stride = _rows_f16(qkv, T, (c.n_heads + 2 * c.n_kv_heads) * c.head_dim, dev, "qkv")
+        a.q_out, a.q_stride = _rows_f16(q_out, T, c.n_heads * c.head_dim, dev, "q_out")
+        for gain, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+            if gain is not None and (gain.dtype != torch.bfloat16 or gain.device != dev or gain.shape != (c.head_dim,) or
+                                     not gain.is_contiguous()):
+                raise ValueError(f"{name}: a bf16 tensor [{c.head_dim}] on {dev}")
+        a.q_gain = q_norm.data_ptr() if q_norm is not None else None
+        a.k_gain = k_norm.data_ptr() if k_norm is not None else None
+        a.norm_eps = norm_eps
+        if rope is not None:
+            if rope.cos.device != dev:
+                raise ValueError(f"rope: tables on {dev}")
+            a.rope_cos, a.rope_sin = rope.cos.data_ptr(), rope.sin.data_ptr()
+            a.rope_rows, a.rot_dim, a.rope_layout = rope.cos.shape[0], 2 * rope.cos.shape[1], rope.layout
+        check(lib.hb_kv8_append(self.handle, kv.handle, layer, C.byref(rows.struct), C.byref(a), _stream_ptr(stream)),
+              "hb_kv8_append")
+
+    def kv8_attention(self, kv, layer, rows, q, out, scale=0.0, stream=None):
+        """hb_kv8_attention: causal attention of every row of `rows` over its request's pages of layer `layer` of a
+        KvCache8; q and out fp16 [T, Hq Dh] (rows may be strided views); scale 0 = 1 / sqrt(Dh).  The
+        workspace of the call comes from torch's allocator, on the stream of the call."""
+        c = self.cfg
+        T, dev = rows.struct.n_rows, self._same_device(rows, kv)
+        qp, qs = _rows_f16(q, T, c.n_heads * c.head_dim, dev, "q")
+        op, os_ = _rows_f16(out, T, c.n_heads * c.head_dim, dev, "out")
+        need = C.c_size_t()
+        check(lib.hb_kv8_attention_workspace(C.byref(c), C.byref(rows.struct), C.byref(need)), "hb_kv8_attention_workspace")
+        ws = None
+        if need.value:   # allocated on the stream of the call, whose order then protects its reuse
+            with torch.cuda.stream(stream):
+                ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        check(lib.hb_kv8_attention(self.handle, kv.handle, layer, C.byref(rows.struct), qp, qs, op, os_, scale,
+                                   C.c_void_p(ws.data_ptr()) if ws is not None else None, need.value, _stream_ptr(stream)),
+              "hb_kv8_attention")
 
     def status_poll(self, stream=None):
         """Synchronises the stream; returns the device status code (0 = clean)."""

@@ -82,6 +82,7 @@ struct hb_kv {
   hb_model_cfg cfg;
   CUtensorMap map;      // arena as a 2-D tensor [rows of 64 fp16], box = the K+V block of one (page, kv head)
   bool has_map;
+  bool e4m3;            // 8-bit format (hb_kv8_create); has no tensor map
   void* arena;
   size_t arena_bytes;
   int32_t n_pages;
@@ -213,6 +214,14 @@ int hb_launch_wait_expiry_selftest(hb_ctx* c, uint64_t limit_ns, cudaStream_t s)
 int hb_launch_pool_chunk(hb_ctx* c, const float* x, const void* gain, int n_rows, int mode, int first_chunk,
                          int is_final, float* slot_sum, uint32_t* slot_meta, float* out_emb, cudaStream_t s);
 int hb_launch_bf16_to_f16(const void* src, void* dst, size_t n, cudaStream_t s);
+
+// 8-bit KV cache (kv8_append.cu, kv8_attention.cu)
+namespace hb_kv8 { struct Rows; }
+int hb_launch_kv8_append(hb_ctx* c, const hb_kv8::Rows& r, const hb_append_args& a, cudaStream_t s, bool pdl);
+int hb_launch_kv8_attention(hb_ctx* c, const hb_kv8::Rows& r, const void* q, int64_t q_stride, void* out, int64_t out_stride,
+                            float scale, void* workspace, cudaStream_t s, bool pdl);
+size_t hb_kv8_attention_scratch(int n_segs, int n_kv_heads, int head_dim, int max_keys);   // bytes of workspace
+int hb_kv8_max_segs();
 
 struct hb_ctx {
   hb_model_cfg cfg;

@@ -8,6 +8,7 @@
 #include <new>
 
 #include "hb_internal.h"
+#include "kv8.cuh"
 
 namespace {
 
@@ -390,6 +391,7 @@ int hb_kv_create(const hb_model_cfg* cfg, void* arena, size_t arena_bytes, int32
   if (!kv) return HB_ERR_BAD_ARG;
   kv->cfg = *cfg;
   kv->has_map = false;
+  kv->e4m3 = false;
   if (arena) {
     // arena as rows of 64 elements; one copy box = the K+V block of one (page, kv head)
     const uint64_t halves = cfg->head_dim / 64;
@@ -405,6 +407,37 @@ int hb_kv_create(const hb_model_cfg* cfg, void* arena, size_t arena_bytes, int32
   kv->arena_bytes = arena_bytes;
   kv->n_pages = n_pages;
   kv->used.assign(n_pages, 0);
+  kv->n_free = n_pages;
+  *out = kv;
+  return HB_OK;
+}
+
+int hb_kv8_arena_bytes(const hb_model_cfg* cfg, int32_t n_pages, size_t* out_bytes) {
+  if (!cfg_ok(cfg) || n_pages < 1 || !out_bytes) return HB_ERR_BAD_ARG;
+  *out_bytes = static_cast<size_t>(cfg->n_layers) * n_pages * cfg->n_kv_heads * hb_kv8::block_bytes(cfg->head_dim);
+  return HB_OK;
+}
+
+int hb_kv8_create(const hb_model_cfg* cfg, void* arena, size_t arena_bytes, int32_t n_pages, hb_kv** out) {
+  if (!out) return HB_ERR_BAD_ARG;
+  *out = nullptr;
+  size_t need = 0;
+  if (hb_kv8_arena_bytes(cfg, n_pages, &need) != HB_OK) return HB_ERR_BAD_ARG;
+  if (arena && (arena_bytes < need || misaligned(arena, 256))) return HB_ERR_BAD_ARG;
+  hb_kv* kv = new (std::nothrow) hb_kv();
+  if (!kv) return HB_ERR_BAD_ARG;
+  kv->cfg = *cfg;
+  kv->has_map = false;
+  kv->e4m3 = true;
+  kv->arena = arena;
+  kv->arena_bytes = arena_bytes;
+  kv->n_pages = n_pages;
+  try {
+    kv->used.assign(n_pages, 0);
+  } catch (...) {   // out of host memory
+    delete kv;
+    return HB_ERR_BAD_ARG;
+  }
   kv->n_free = n_pages;
   *out = kv;
   return HB_OK;
@@ -512,6 +545,116 @@ int hb_pool_free_slot(hb_pool* p, int32_t slot) {
   if (!p || slot < 0 || slot >= p->n_slots || !p->used[slot]) return HB_ERR_BAD_ARG;
   p->used[slot] = 0;
   ++p->n_free;
+  return HB_OK;
+}
+
+// ---- operators over the 8-bit cache ------------------------------------------------
+
+}  // extern "C"
+
+namespace {
+
+bool same_cfg(const hb_model_cfg& a, const hb_model_cfg& b) { return memcmp(&a, &b, sizeof(hb_model_cfg)) == 0; }
+
+// What both operators check of the cache, the layer and the rows, and the kernels' view of them.
+int kv8_rows(hb_ctx* c, hb_kv* kv, int32_t layer, const hb_rows* r, hb_kv8::Rows* out) {
+  if (!c || !kv || !r) return HB_ERR_BAD_ARG;
+  if (!kv->e4m3 || !kv->arena || !same_cfg(kv->cfg, c->cfg)) return HB_ERR_BAD_ARG;
+  if (layer < 0 || layer >= c->cfg.n_layers) return HB_ERR_BAD_ARG;
+  if (r->n_segs < 0 || r->n_page_ids < 0 || r->n_rows < 0 || r->max_q_len < 0 || r->max_keys < 0) return HB_ERR_BAD_ARG;
+  if (r->n_segs > hb_kv8_max_segs()) return HB_ERR_TOO_LARGE;
+  if ((r->n_segs > 0 && !r->segs) || (r->n_page_ids > 0 && !r->page_ids) || (r->n_rows > 0 && !r->row_seg)) return HB_ERR_BAD_ARG;
+  if (misaligned(r->segs, 16) || misaligned(r->page_ids, 4) || misaligned(r->row_seg, 4)) return HB_ERR_BAD_ARG;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return HB_ERR_CUDA;
+  if (dev != c->device) return HB_ERR_BAD_ARG;   // launches go to the current device
+  out->segs = r->segs;
+  out->page_ids = r->page_ids;
+  out->row_seg = r->row_seg;
+  out->n_segs = r->n_segs;
+  out->n_page_ids = r->n_page_ids;
+  out->n_rows = r->n_rows;
+  out->max_q_len = r->max_q_len;
+  out->max_keys = r->max_keys;
+  out->n_pages = kv->n_pages;
+  out->Hkv = c->cfg.n_kv_heads;
+  out->G = c->cfg.n_heads / c->cfg.n_kv_heads;
+  out->page_stride = static_cast<int64_t>(c->cfg.n_kv_heads) * static_cast<int64_t>(hb_kv8::block_bytes(c->cfg.head_dim));
+  out->arena = static_cast<uint8_t*>(kv->arena) + layer * out->page_stride * kv->n_pages;
+  out->status = c->status;
+  return HB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int hb_kv8_append(hb_ctx* c, hb_kv* kv, int32_t layer, const hb_rows* rows, const hb_append_args* a, void* stream) {
+  hb_kv8::Rows r;
+  const int rc = kv8_rows(c, kv, layer, rows, &r);
+  if (rc != HB_OK) return rc;
+  if (!a) return HB_ERR_BAD_ARG;
+  if (a->rot_dim < 0 || a->rot_dim > c->cfg.head_dim || a->rot_dim % 16) return HB_ERR_BAD_ARG;
+  if (a->rope_layout != HB_ROPE_PAIRS && a->rope_layout != HB_ROPE_HALVES) return HB_ERR_BAD_ARG;
+  if (a->rot_dim > 0 && (!a->rope_cos || !a->rope_sin || a->rope_rows < 1)) return HB_ERR_BAD_ARG;
+  if ((a->q_gain || a->k_gain) && !(a->norm_eps >= 0.0f)) return HB_ERR_BAD_ARG;
+  const int64_t n_q = static_cast<int64_t>(c->cfg.n_heads) * c->cfg.head_dim;
+  const int64_t n_qkv = n_q + 2ll * c->cfg.n_kv_heads * c->cfg.head_dim;
+  if (a->qkv_stride < n_qkv || a->qkv_stride % 8 || a->q_stride < n_q || a->q_stride % 8) return HB_ERR_BAD_ARG;
+  if (misaligned(a->qkv, 16) || misaligned(a->q_out, 16) || misaligned(a->q_gain, 16) || misaligned(a->k_gain, 16) ||
+      misaligned(a->rope_cos, 16) || misaligned(a->rope_sin, 16))
+    return HB_ERR_BAD_ARG;
+  if (r.n_rows == 0) return HB_OK;
+  if (!a->qkv || !a->q_out) return HB_ERR_BAD_ARG;
+  return hb_launch_kv8_append(c, r, *a, static_cast<cudaStream_t>(stream), false);
+}
+
+int hb_kv8_attention_workspace(const hb_model_cfg* cfg, const hb_rows* rows, size_t* out_bytes) {
+  if (!cfg_ok(cfg) || !rows || !out_bytes || rows->n_segs < 0 || rows->max_keys < 0) return HB_ERR_BAD_ARG;
+  if (rows->n_segs > hb_kv8_max_segs()) return HB_ERR_TOO_LARGE;
+  *out_bytes = hb_kv8_attention_scratch(rows->n_segs, cfg->n_kv_heads, cfg->head_dim, rows->max_keys);
+  return HB_OK;
+}
+
+int hb_kv8_attention(hb_ctx* c, hb_kv* kv, int32_t layer, const hb_rows* rows, const void* q, int64_t q_stride, void* out,
+                     int64_t out_stride, float scale, void* workspace, size_t workspace_bytes, void* stream) {
+  hb_kv8::Rows r;
+  const int rc = kv8_rows(c, kv, layer, rows, &r);
+  if (rc != HB_OK) return rc;
+  const int64_t n_q = static_cast<int64_t>(c->cfg.n_heads) * c->cfg.head_dim;
+  if (q_stride < n_q || q_stride % 8 || out_stride < n_q || out_stride % 8) return HB_ERR_BAD_ARG;
+  if (misaligned(q, 16) || misaligned(out, 16)) return HB_ERR_BAD_ARG;
+  if (!(scale >= 0.0f) || !(scale <= 3.0e38f)) return HB_ERR_BAD_ARG;
+  const size_t need = hb_kv8_attention_scratch(r.n_segs, r.Hkv, c->cfg.head_dim, r.max_keys);
+  if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 256))) return HB_ERR_BAD_ARG;
+  if (r.n_rows == 0 || r.n_segs == 0 || r.max_q_len == 0) return HB_OK;
+  if (!q || !out) return HB_ERR_BAD_ARG;
+  if (scale == 0.0f) scale = 1.0f / sqrtf(static_cast<float>(c->cfg.head_dim));
+  return hb_launch_kv8_attention(c, r, q, q_stride, out, out_stride, scale, workspace, static_cast<cudaStream_t>(stream), false);
+}
+
+int hb_rope_table(int32_t n_pos, int32_t rot_dim, double theta, const hb_rope_scaling* sc, float* out_cos, float* out_sin) {
+  if (n_pos < 1 || rot_dim < 2 || rot_dim % 2 || !(theta > 0.0) || !out_cos || !out_sin) return HB_ERR_BAD_ARG;
+  if (sc) {
+    if (sc->kind != HB_ROPE_LINEAR && sc->kind != HB_ROPE_BY_PARTS) return HB_ERR_BAD_ARG;
+    if (!(sc->factor >= 1.0) || !(sc->attn_factor > 0.0)) return HB_ERR_BAD_ARG;
+    if (sc->kind == HB_ROPE_BY_PARTS && (!(sc->orig_len > 0.0) || !(sc->lo >= 0.0) || !(sc->hi > sc->lo))) return HB_ERR_BAD_ARG;
+  }
+  const int half = rot_dim / 2;
+  const double mul = sc ? sc->attn_factor : 1.0;
+  for (int i = 0; i < half; ++i) {
+    double f = pow(theta, -2.0 * i / rot_dim);
+    if (sc && sc->kind == HB_ROPE_LINEAR) f /= sc->factor;
+    if (sc && sc->kind == HB_ROPE_BY_PARTS) {
+      const double turns = sc->orig_len * f / 6.283185307179586476925;
+      const double g = std::min(1.0, std::max(0.0, (turns - sc->lo) / (sc->hi - sc->lo)));
+      f *= g + (1.0 - g) / sc->factor;
+    }
+    for (int p = 0; p < n_pos; ++p) {
+      out_cos[static_cast<size_t>(p) * half + i] = static_cast<float>(mul * cos(p * f));
+      out_sin[static_cast<size_t>(p) * half + i] = static_cast<float>(mul * sin(p * f));
+    }
+  }
   return HB_OK;
 }
 

@@ -1,0 +1,527 @@
+// Attention over the 8-bit paged KV cache (causal, grouped query heads, ragged segments).
+//
+//   s_ij = scale * q_i . k_j (j <= pos_i);  o_i = sum_j softmax(s_i)_j v_j
+//
+// Items.  The q_len * G rows a segment has for one KV head (G = Hq / Hkv; column c = row c / G, head c % G)
+// are cut into column tiles of 16; a segment of one tile (decode rows) has its keys cut into splits,
+// whose number depends on the segment's own length only.  Each block walks items b, b + grid, ...; the
+// segment of an item is found in a prefix sum over the segments that the block forms itself, so that
+// nothing about the batch has to be known on the host and a captured launch follows the arrays.
+//
+// One item: four warps share the columns and take every fourth page.  A warp fetches a page's block of
+// this KV head (K, V and scales: 2 - 4 KiB, contiguous) with one bulk copy into its own ring and
+// computes transposed, so that the 16 keys of the page fill the 16 rows of the matrix instruction
+// whatever G is:
+//   S^T[16 keys, 8 cols] = K[16, DH] Q^T          A = codes of K converted to fp16 (exact), B = q
+//   O^T[DH, 8 cols]     += V^T[DH, 16] P^T[16, 8]  A = codes of V, B = P^T (one 8 x 8 transpose per 8 keys)
+// The scale of K multiplies the fp32 scores.  The scale 2^e of V is folded into the exponent: P holds
+// 2^(s - m + e) with m the running maximum of s + e over the keys, and the sum takes 2^-e back out, so
+// neither scale is ever rounded.
+#include <algorithm>
+
+#include "kv8.cuh"
+
+namespace {
+
+using namespace hb_kv8;
+
+constexpr int DEC_WARPS = 4;
+constexpr int DEC_THREADS = DEC_WARPS * 32;
+constexpr int STAGES = 3;
+constexpr int TILE_COLS = 16;
+constexpr int MIN_SPLIT_KEYS = 512, MAX_SPLITS = 64;
+constexpr int MAX_SEGS = 8192;
+constexpr uint64_t WAIT_NS = 1000000000ull;
+
+struct AttnParams {
+  Rows r;
+  const __half* q;
+  __half* out;
+  int64_t q_stride, out_stride;
+  float scale_log2;
+  int32_t max_splits;   // splits of the longest segment
+  float* part_o;        // [n_segs * Hkv][max_splits][16][DH]: weighted sums relative to their maximum
+  float2* part_ml;      // [n_segs * Hkv][max_splits][16]: maximum (log2), sum
+};
+
+// Keys per split of a segment with `keys` keys: 512, more once that would be over MAX_SPLITS splits (whole
+// pages for each warp).
+__device__ __forceinline__ int split_keys(int keys) {
+  const int per = (keys / MAX_SPLITS + 128) / 128 * 128;
+  return per < MIN_SPLIT_KEYS ? MIN_SPLIT_KEYS : per;
+}
+__device__ __forceinline__ int n_splits(int keys) {
+  const int per = split_keys(keys);
+  return keys <= per ? 1 : (keys - 1) / per + 1;
+}
+// No segment of up to max_keys keys has more splits (the count itself is not monotonic in the keys).
+inline int splits_bound(int max_keys) { return std::max(1, std::min(MAX_SPLITS, max_keys / MIN_SPLIT_KEYS + 1)); }
+
+struct Seg { int q_start, q_len, pos_start, pt_start; };
+
+__device__ __forceinline__ bool load_seg(const Rows& r, int s, Seg& g) {
+  const int4 a = __ldg(reinterpret_cast<const int4*>(r.segs + s));
+  const int4 b = __ldg(reinterpret_cast<const int4*>(r.segs + s) + 1);
+  g.q_start = a.y; g.q_len = a.z; g.pos_start = a.w; g.pt_start = b.x;
+  return seg_ok(r, g.q_start, g.q_len, g.pos_start, g.pt_start, b.y);
+}
+
+// Items of a segment: column tiles x splits (only one-tile segments are split), times the KV heads.
+__device__ __forceinline__ int tiles_of(const Rows& r, const Seg& g) { return (g.q_len * r.G + TILE_COLS - 1) / TILE_COLS; }
+__device__ __forceinline__ int splits_of(int tiles, const Seg& g) { return tiles == 1 ? n_splits(g.pos_start + g.q_len) : 1; }
+
+struct Item {
+  Seg g;
+  int seg, head, tile, split, ns;
+  int col0, n_cols;   // columns of this tile
+  int key0, key1;     // keys [key0, key1) that some column of the tile may see
+};
+
+__device__ __forceinline__ void find_item(const AttnParams& p, const int* prefix, int idx, Item& it) {
+  int lo = 0, hi = p.r.n_segs;   // prefix[lo] <= idx < prefix[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (prefix[mid] <= idx) lo = mid; else hi = mid;
+  }
+  it.seg = lo;
+  load_seg(p.r, lo, it.g);
+  const int tiles = tiles_of(p.r, it.g), keys = it.g.pos_start + it.g.q_len;
+  it.ns = splits_of(tiles, it.g);
+  int at = idx - prefix[lo];
+  it.head = at % p.r.Hkv;
+  at /= p.r.Hkv;
+  it.split = at % it.ns;
+  it.tile = at / it.ns;
+  it.col0 = it.tile * TILE_COLS;
+  it.n_cols = min(TILE_COLS, it.g.q_len * p.r.G - it.col0);
+  const int seen = it.g.pos_start + (it.col0 + it.n_cols - 1) / p.r.G + 1;
+  const int per = it.ns > 1 ? split_keys(keys) : keys;
+  it.key0 = it.split * per;
+  it.key1 = min(seen, it.key0 + per);
+}
+
+// prefix[s] = items before segment s; returns the total.  All threads; ends with a barrier.
+__device__ int build_prefix(const AttnParams& p, int* prefix, int* warp_sums) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.r.n_segs;
+  const int per = (n + DEC_THREADS - 1) / DEC_THREADS, from = min(n, tid * per), to = min(n, from + per);
+  int sum = 0;
+  for (int s = from; s < to; ++s) {
+    Seg g;
+    int items = 0;
+    if (load_seg(p.r, s, g)) {
+      const int tiles = tiles_of(p.r, g);
+      items = tiles * splits_of(tiles, g) * p.r.Hkv;
+    } else if (blockIdx.x == 0) {
+      atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
+    }
+    prefix[s] = sum;
+    sum += items;
+  }
+  int incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 31) warp_sums[warp] = incl;
+  __syncthreads();
+  int base = incl - sum, total = 0;
+#pragma unroll
+  for (int w = 0; w < DEC_WARPS; ++w) {
+    if (w < warp) base += warp_sums[w];
+    total += warp_sums[w];
+  }
+  for (int s = from; s < to; ++s) prefix[s] += base;
+  if (tid == 0) prefix[n] = total;
+  __syncthreads();
+  return total;
+}
+
+template <int DH>
+struct DecCfg {
+  static constexpr int BLK = Block<DH>::BYTES;
+  static constexpr int RING = DEC_WARPS * STAGES * BLK;
+  static constexpr int ROW = DH + 4;   // floats per column of the merge buffer (the odd quarter keeps the stores conflict-free)
+  static constexpr int MERGE = DEC_WARPS * 8 * ROW * 4;          // one 8-column tile at a time
+  static constexpr int ML = DEC_WARPS * TILE_COLS * 8;
+  static constexpr int BARS = DEC_WARPS * STAGES * 8;
+  static constexpr int FIXED = RING + MERGE + ML + BARS + 64;
+};
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+// What a warp keeps of its columns: the lane holds columns 8 nt + 2t and 8 nt + 2t + 1.
+template <int DH, int NT>
+struct State {
+  uint32_t q[NT][DH / 16][2];
+  float o[NT][DH / 16][4];
+  float m[NT][2], l[NT][2];
+  int lim[NT][2];   // last visible key of the lane's columns, -1 for unused ones
+};
+
+template <int DH, int NT>
+__device__ __forceinline__ void begin(const AttnParams& p, const Item& it, State<DH, NT>& st) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int c = nt * 8 + g;
+    const int col = it.col0 + min(c, it.n_cols - 1);
+    const __half* src = p.q + (it.g.q_start + col / p.r.G) * p.q_stride + (it.head * p.r.G + col % p.r.G) * DH + t * 16;
+#pragma unroll
+    for (int hf = 0; hf < DH / 64; ++hf) {
+      uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+      if (c < it.n_cols) {
+        a = __ldg(reinterpret_cast<const uint4*>(src + hf * 64));
+        b = __ldg(reinterpret_cast<const uint4*>(src + hf * 64) + 1);
+      }
+      st.q[nt][hf * 4 + 0][0] = a.x; st.q[nt][hf * 4 + 0][1] = a.y;
+      st.q[nt][hf * 4 + 1][0] = a.z; st.q[nt][hf * 4 + 1][1] = a.w;
+      st.q[nt][hf * 4 + 2][0] = b.x; st.q[nt][hf * 4 + 2][1] = b.y;
+      st.q[nt][hf * 4 + 3][0] = b.z; st.q[nt][hf * 4 + 3][1] = b.w;
+    }
+#pragma unroll
+    for (int mt = 0; mt < DH / 16; ++mt) st.o[nt][mt][0] = st.o[nt][mt][1] = st.o[nt][mt][2] = st.o[nt][mt][3] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int cc = nt * 8 + 2 * t + e;
+      st.m[nt][e] = -INFINITY;
+      st.l[nt][e] = 0.0f;
+      st.lim[nt][e] = cc < it.n_cols ? min(it.key1 - 1, it.g.pos_start + (it.col0 + cc) / p.r.G) : -1;
+    }
+  }
+}
+
+// One page (16 keys from `key`) out of shared memory at `blk`.
+template <int DH, int NT>
+__device__ __forceinline__ void page_step(const AttnParams& p, const Item& it, uint32_t blk, int key, State<DH, NT>& st) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  float ks, vs;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks), "=f"(vs) : "r"(blk + Block<DH>::HDR));
+  ks *= p.scale_log2;
+  const int ev = exponent_of(vs);
+  const float fev = static_cast<float>(ev), back = pow2f(max(-126, min(126, -ev)));
+  float s[NT][4];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
+#pragma unroll
+  for (int hf = 0; hf < DH / 64; ++hf) {
+    const uint4 ka = lds128(blk + hf * 1024 + g * 64 + t * 16), kb = lds128(blk + hf * 1024 + (g + 8) * 64 + t * 16);
+    const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      uint32_t a[4];
+      e4m3x4_to_half2x2(wa[w], a[0], a[2]);
+      e4m3x4_to_half2x2(wb[w], a[1], a[3]);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], a, st.q[nt][hf * 4 + w][0], st.q[nt][hf * 4 + w][1]);
+    }
+  }
+  // scores in the log2 domain, plus V's exponent; invisible keys -inf
+  bool grow = false;
+  float mx[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const bool v0 = key + g <= st.lim[nt][e], v1 = key + g + 8 <= st.lim[nt][e];
+      s[nt][e] = v0 ? fmaf(s[nt][e], ks, fev) : -INFINITY;
+      s[nt][2 + e] = v1 ? fmaf(s[nt][2 + e], ks, fev) : -INFINITY;
+      float m = fmaxf(s[nt][e], s[nt][2 + e]);
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+      mx[nt][e] = m;
+      grow |= m > st.m[nt][e] + 13.0f || (st.m[nt][e] == -INFINITY && m > -INFINITY);
+    }
+  }
+  // The reference maximum moves only when a column's maximum has grown by more than 2^13 over it.  It is
+  // kept 6 below the maximum it was taken from, so that P lies in (0, 2^15): the small probabilities of a
+  // long context stay normal fp16 numbers down to 2^-20 of the largest.
+  if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float f[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float m_new = mx[nt][e] - 6.0f;
+        const bool up = mx[nt][e] > -INFINITY && !(m_new <= st.m[nt][e]);
+        f[e] = up ? ex2_approx(st.m[nt][e] - m_new) : 1.0f;   // -inf -> 0
+        if (up) st.m[nt][e] = m_new;
+        st.l[nt][e] *= f[e];
+      }
+#pragma unroll
+      for (int mt = 0; mt < DH / 16; ++mt) {
+        st.o[nt][mt][0] *= f[0]; st.o[nt][mt][1] *= f[1];
+        st.o[nt][mt][2] *= f[0]; st.o[nt][mt][3] *= f[1];
+      }
+    }
+  }
+  uint32_t pt[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float w[4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float m = st.m[nt][e] == -INFINITY ? 0.0f : st.m[nt][e];
+      w[e] = ex2_approx(s[nt][e] - m);
+      w[2 + e] = ex2_approx(s[nt][2 + e] - m);
+      st.l[nt][e] = fmaf(w[e] + w[2 + e], back, st.l[nt][e]);
+    }
+    pt[nt][0] = transpose8x8(pack_half2(w[0], w[1]));
+    pt[nt][1] = transpose8x8(pack_half2(w[2], w[3]));
+  }
+  // tokens past the request's last key hold whatever was there: their codes become zero (0 * NaN is NaN)
+  uint32_t keep = 0xffffffffu;
+  const int left = it.g.pos_start + it.g.q_len - key;
+  if (left < PAGE) {
+    keep = (2 * t < left ? 0xffu : 0u) | (2 * t + 1 < left ? 0xff00u : 0u) | (2 * t + 8 < left ? 0xff0000u : 0u) |
+           (2 * t + 9 < left ? 0xff000000u : 0u);
+  }
+#pragma unroll
+  for (int c = 0; c < DH / 32; ++c) {
+    const uint4 v = lds128(blk + Block<DH>::V_OFF + c * 512 + lane * 16);
+    const uint32_t wv[4] = {v.x & keep, v.y & keep, v.z & keep, v.w & keep};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t a[4];
+      e4m3x4_to_half2x2(wv[2 * h], a[0], a[2]);
+      e4m3x4_to_half2x2(wv[2 * h + 1], a[1], a[3]);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) mma_f16(st.o[nt][c * 2 + h], a, pt[nt][0], pt[nt][1]);
+    }
+  }
+}
+
+// A warp's ring of page blocks.  n counts the copies asked for, c those consumed, over the block's life.
+struct Ring {
+  uint32_t buf, bar;
+  uint32_t n, c;
+};
+
+template <int DH>
+__device__ __forceinline__ void request(const AttnParams& p, Ring& ring, int page, int head) {
+  // every lane; lane 0 issues
+  const uint32_t st = ring.n % STAGES;
+  if ((threadIdx.x & 31) == 0) {
+    const uint32_t bar = ring.bar + 8u * st;
+    mbar_arrive_expect_tx(bar, Block<DH>::BYTES);
+    bulk_load(ring.buf + st * Block<DH>::BYTES,
+              p.r.arena + page * p.r.page_stride + static_cast<int64_t>(head) * Block<DH>::BYTES, Block<DH>::BYTES, bar);
+  }
+  ++ring.n;
+}
+
+template <int DH, int NT>
+__device__ __forceinline__ bool run_item(const AttnParams& p, const Item& it, Ring& ring, uint8_t* smem, volatile uint32_t* abort_flag) {
+  using C = DecCfg<DH>;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  State<DH, NT> st;
+  begin<DH, NT>(p, it, st);
+  const int pg0 = it.key0 / PAGE, pg1 = (it.key1 + PAGE - 1) / PAGE;
+  const int mine = pg1 - pg0 > warp ? (pg1 - pg0 - warp + DEC_WARPS - 1) / DEC_WARPS : 0;
+  bool ok = true;
+  for (int batch = 0; batch < mine && ok; batch += 32) {
+    // page ids of the warp's next 32 pages, one per lane
+    const int nb = min(32, mine - batch);
+    int id = -1;
+    if (lane < nb) id = __ldg(p.r.page_ids + it.g.pt_start + pg0 + warp + (batch + lane) * DEC_WARPS);
+    if (__any_sync(0xffffffffu, lane < nb && (id < 0 || id >= p.r.n_pages))) {
+      if (lane == 0) atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
+      ok = false;
+      break;
+    }
+    int asked = 0;
+    for (; asked < min(nb, STAGES); ++asked) request<DH>(p, ring, __shfl_sync(0xffffffffu, id, asked), it.head);
+    for (int i = 0; i < nb; ++i) {
+      const uint32_t sg = ring.c % STAGES;
+      if (!__all_sync(0xffffffffu, mbar_wait(ring.bar + 8u * sg, (ring.c / STAGES) & 1u, abort_flag, WAIT_NS))) { ok = false; break; }
+      page_step<DH, NT>(p, it, ring.buf + sg * Block<DH>::BYTES, (pg0 + warp + (batch + i) * DEC_WARPS) * PAGE, st);
+      ++ring.c;
+      __syncwarp();   // every lane has read the stage
+      if (asked < nb) { request<DH>(p, ring, __shfl_sync(0xffffffffu, id, asked), it.head); ++asked; }
+    }
+  }
+  // ---- join the four warps: common maximum, then the weighted sums through shared memory ----
+  float* merge = reinterpret_cast<float*>(smem + C::RING);
+  float2* ml = reinterpret_cast<float2*>(smem + C::RING + C::MERGE);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float l = st.l[nt][e];
+      l += __shfl_xor_sync(0xffffffffu, l, 4);
+      l += __shfl_xor_sync(0xffffffffu, l, 8);
+      l += __shfl_xor_sync(0xffffffffu, l, 16);
+      if (g == 0) ml[warp * TILE_COLS + nt * 8 + 2 * t + e] = make_float2(st.m[nt][e], l);
+    }
+  const bool all_ok = __syncthreads_and(ok) != 0;
+  if (!all_ok && it.ns > 1 && tid < it.n_cols)   // a negative sum tells the join to leave the row alone
+    p.part_ml[((static_cast<int64_t>(it.seg) * p.r.Hkv + it.head) * p.max_splits + it.split) * TILE_COLS + tid] = make_float2(-INFINITY, -1.0f);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float f[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < DEC_WARPS; ++w) m = fmaxf(m, ml[w * TILE_COLS + nt * 8 + 2 * t + e].x);
+      f[e] = st.m[nt][e] == -INFINITY ? 0.0f : ex2_approx(st.m[nt][e] - m);
+    }
+    float* mine_at = merge + (warp * 8 + 2 * t) * C::ROW + g;
+#pragma unroll
+    for (int mt = 0; mt < DH / 16; ++mt) {
+      mine_at[mt * 16] = st.o[nt][mt][0] * f[0];
+      mine_at[C::ROW + mt * 16] = st.o[nt][mt][1] * f[1];
+      mine_at[mt * 16 + 8] = st.o[nt][mt][2] * f[0];
+      mine_at[C::ROW + mt * 16 + 8] = st.o[nt][mt][3] * f[1];
+    }
+    __syncthreads();
+    if (all_ok) {
+      // two neighbouring dimensions per thread
+      for (int u = tid; u < 8 * (DH / 2); u += DEC_THREADS) {
+        const int cc = u / (DH / 2), d = (u % (DH / 2)) * 2, c = nt * 8 + cc;
+        if (c >= it.n_cols) continue;
+        float m = -INFINITY, l = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+        for (int w = 0; w < DEC_WARPS; ++w) m = fmaxf(m, ml[w * TILE_COLS + c].x);
+#pragma unroll
+        for (int w = 0; w < DEC_WARPS; ++w) {
+          const float2 a = ml[w * TILE_COLS + c];
+          if (a.x > -INFINITY) l = fmaf(a.y, ex2_approx(a.x - m), l);
+          const float2 b = *reinterpret_cast<const float2*>(merge + (w * 8 + cc) * C::ROW + d);
+          x += b.x;
+          y += b.y;
+        }
+        if (it.ns == 1) {
+          const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+          const int col = it.col0 + c;
+          __half* dst = p.out + (it.g.q_start + col / p.r.G) * p.out_stride + (it.head * p.r.G + col % p.r.G) * DH + d;
+          *reinterpret_cast<uint32_t*>(dst) = pack_half2_sat(x * inv, y * inv);
+        } else {
+          const int64_t rec = (static_cast<int64_t>(it.seg) * p.r.Hkv + it.head) * p.max_splits + it.split;
+          *reinterpret_cast<float2*>(p.part_o + (rec * TILE_COLS + c) * DH + d) = make_float2(x, y);
+          if (d == 0) p.part_ml[rec * TILE_COLS + c] = make_float2(m, l);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  return all_ok;
+}
+
+template <int DH>
+__global__ void __launch_bounds__(DEC_THREADS, 3)
+kv8_attend_kernel(const AttnParams p) {
+  grid_dep_wait();
+  using C = DecCfg<DH>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int tid = threadIdx.x, warp = tid >> 5;
+  uint8_t* tail = smem + C::RING + C::MERGE + C::ML;
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(tail + C::BARS);
+  int* warp_sums = reinterpret_cast<int*>(tail + C::BARS + 16);
+  int* prefix = reinterpret_cast<int*>(smem + C::FIXED);
+  Ring ring;
+  ring.buf = smem_u32(smem) + warp * STAGES * C::BLK;
+  ring.bar = smem_u32(tail) + warp * STAGES * 8;
+  ring.n = ring.c = 0;
+  if (tid < DEC_WARPS * STAGES) mbar_init(smem_u32(tail) + 8u * tid, 1);
+  if (tid == 0) *abort_flag = 0u;
+  mbar_init_fence();
+  const int total = build_prefix(p, prefix, warp_sums);   // its barriers publish the initialisation
+  for (int idx = blockIdx.x; idx < total; idx += gridDim.x) {
+    Item it;
+    find_item(p, prefix, idx, it);
+    const bool ok = it.n_cols <= 8 ? run_item<DH, 1>(p, it, ring, smem, abort_flag) : run_item<DH, 2>(p, it, ring, smem, abort_flag);
+    if (*abort_flag) {
+      // a wait ran out: report, let requested copies land, leave
+      if (tid == 0) {
+        atomicOr(p.r.status, HB_DEV_ATTN_WAIT_EXPIRED);
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);
+      }
+      __syncthreads();
+      break;
+    }
+    (void)ok;   // a bad page id costs this item only (nothing of it is in flight: ids are checked before the copies)
+  }
+  grid_dep_launch();
+}
+
+// Joins the splits of one (segment, KV head, column): thread = dimension, split order fixed.
+template <int DH>
+__global__ void __launch_bounds__(DH)
+kv8_join_kernel(const AttnParams p, const int cols) {
+  grid_dep_wait();
+  const int c = blockIdx.x % cols, head = (blockIdx.x / cols) % p.r.Hkv, seg = blockIdx.x / (cols * p.r.Hkv);
+  Seg g;
+  if (!load_seg(p.r, seg, g)) return;
+  const int tiles = tiles_of(p.r, g), ns = splits_of(tiles, g);
+  if (tiles != 1 || ns == 1 || c >= g.q_len * p.r.G) return;
+  const int64_t rec = (static_cast<int64_t>(seg) * p.r.Hkv + head) * p.max_splits;
+  float m = -INFINITY;
+  for (int s = 0; s < ns; ++s) {
+    const float2 a = p.part_ml[(rec + s) * TILE_COLS + c];
+    if (a.y < 0.0f) return;   // a split that was given up
+    m = fmaxf(m, a.x);
+  }
+  float l = 0.0f, x = 0.0f;
+#pragma unroll 8
+  for (int s = 0; s < ns; ++s) {
+    const float2 a = p.part_ml[(rec + s) * TILE_COLS + c];
+    const float f = a.x > -INFINITY ? ex2_approx(a.x - m) : 0.0f;
+    l = fmaf(a.y, f, l);
+    x = fmaf(p.part_o[((rec + s) * TILE_COLS + c) * DH + threadIdx.x], f, x);
+  }
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  p.out[(g.q_start + c / p.r.G) * p.out_stride + (head * p.r.G + c % p.r.G) * DH + threadIdx.x] =
+      __float2half_rn(sat_half_range(x * inv));
+}
+
+template <int DH>
+int launch(const AttnParams& p, int num_sms, cudaStream_t s, bool pdl) {
+  static DynSmemState configured;
+  const int smem = DecCfg<DH>::FIXED + (p.r.n_segs + 1) * 4;
+  if (smem > 227 * 1024) return HB_ERR_TOO_LARGE;
+  auto kern = kv8_attend_kernel<DH>;
+  if (hb_ensure_dyn_smem(reinterpret_cast<const void*>(kern), configured, smem) != HB_OK) return HB_ERR_CUDA;
+  // no more blocks than the bounds of the call allow items
+  const long long tiles = (static_cast<long long>(p.r.max_q_len) * p.r.G + TILE_COLS - 1) / TILE_COLS;
+  const long long most = static_cast<long long>(p.r.n_segs) * p.r.Hkv * std::max<long long>(tiles, p.max_splits);
+  const int blocks = static_cast<int>(std::min<long long>(most, 3ll * num_sms));
+  int rc = hb_launch_kernel(kern, blocks, DEC_THREADS, smem, s, pdl, p);
+  if (rc != HB_OK || p.max_splits == 1) return rc;
+  const int cols = static_cast<int>(std::min<long long>(TILE_COLS, static_cast<long long>(p.r.max_q_len) * p.r.G));
+  return hb_launch_kernel(kv8_join_kernel<DH>, static_cast<unsigned>(p.r.n_segs) * p.r.Hkv * cols, DH, 0, s, true, p, cols);
+}
+
+size_t part_records(int n_segs, int n_kv_heads, int splits) {
+  return splits > 1 ? static_cast<size_t>(n_segs) * n_kv_heads * splits * TILE_COLS : 0;
+}
+
+}  // namespace
+
+int hb_kv8_max_segs() { return MAX_SEGS; }
+
+size_t hb_kv8_attention_scratch(int n_segs, int n_kv_heads, int head_dim, int max_keys) {
+  return part_records(n_segs, n_kv_heads, splits_bound(max_keys)) * (static_cast<size_t>(head_dim) * 4 + 8);
+}
+
+int hb_launch_kv8_attention(hb_ctx* c, const hb_kv8::Rows& r, const void* q, int64_t q_stride, void* out, int64_t out_stride,
+                            float scale, void* workspace, cudaStream_t s, bool pdl) {
+  AttnParams p;
+  p.r = r;
+  p.q = static_cast<const __half*>(q);
+  p.out = static_cast<__half*>(out);
+  p.q_stride = q_stride;
+  p.out_stride = out_stride;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.max_splits = splits_bound(r.max_keys);
+  p.part_o = static_cast<float*>(workspace);
+  p.part_ml = reinterpret_cast<float2*>(p.part_o + part_records(r.n_segs, r.Hkv, p.max_splits) * c->cfg.head_dim);
+  if (c->cfg.head_dim == 64) return launch<64>(p, c->num_sms, s, pdl);
+  if (c->cfg.head_dim == 128) return launch<128>(p, c->num_sms, s, pdl);
+  return HB_ERR_UNSUPPORTED;
+}
