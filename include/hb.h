@@ -313,6 +313,7 @@ enum {
   HB_STATUS_POOL_INDEX = 8,       /* pooler: slot / row buffer out of range                   */
   HB_STATUS_ATTN_WAIT = 16,       /* attention: a pipeline wait expired                       */
   HB_STATUS_SELFTEST_WAIT = 32,   /* hb_selftest_wait_expiry                                  */
+  HB_STATUS_TOKEN_INDEX = 128,    /* hb_logprobs: a token id beyond the vocabulary (its row got NaN) */
   HB_STATUS_F16_RANGE = 64        /* a normed row or a SwiGLU output was NaN or beyond +-65504:
                                      finite values were stored saturated, NaN was stored as NaN */
 };
@@ -572,6 +573,28 @@ typedef struct {
   double attn_factor;   /* > 0 */
 } hb_rope_scaling;
 HB_API int hb_rope_table(int32_t n_pos, int32_t rot_dim, double theta, const hb_rope_scaling* scaling, float* out_cos, float* out_sin);
+
+/* ---- scoring of logits -------------------------------------------------------- */
+
+/* Largest number of alternatives hb_logprobs gives. */
+#define HB_LOGPROBS_MAX_K 32
+enum { HB_DTYPE_F32 = 0, HB_DTYPE_F16 = 1 };
+
+/* Scores logits rows (the sampler's side of Algorithm 1: what hb_argmax decides, this measures).
+ *   logits   device [n_rows, row_stride] of dtype, the first `vocab` of each row count; rows need no
+ *            alignment beyond their type's
+ *   tokens   device int32 [n_rows]: the token whose log probability is asked for; negative = none
+ *            (0 is written); >= vocab: NaN is written and HB_STATUS_TOKEN_INDEX raised
+ *   out_logprob  float [n_rows]: x[token] - log sum exp x
+ *   out_entropy  float [n_rows]: -sum p log p, in nats
+ *   out_top_ids, out_top_logprobs  int32 / float [n_rows, k]: the k largest, best first, the lower
+ *            token first among equals; 0 <= k <= min(vocab, HB_LOGPROBS_MAX_K); unused (may be NULL) if k = 0
+ * tokens and out_logprob (both or neither), and out_entropy, may be NULL.  vocab up to 2^20.  A logit of -inf has probability 0.  A row that
+ * holds NaN or +inf, or nothing but -inf, has no probabilities: its floats become NaN (NaN logits rank last among
+ * the alternatives).  Statistics in fp32; a row's result does not depend on the other rows. */
+HB_API int hb_logprobs(hb_ctx* ctx, const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride,
+                const int32_t* tokens, int32_t k, float* out_logprob, float* out_entropy, int32_t* out_top_ids,
+                float* out_top_logprobs, void* stream);
 
 #ifdef __cplusplus
 }

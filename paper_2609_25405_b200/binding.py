@@ -19,7 +19,7 @@ ERRORS = {0: "HB_OK", -1: "HB_ERR_BAD_ARG", -2: "HB_ERR_CUDA", -3: "HB_ERR_OOM_P
           -7: "HB_ERR_DEVICE_STATUS", -8: "HB_ERR_UNSUPPORTED"}
 from .consts import (KIND_DECODE, KIND_PREFILL_CHUNK, KIND_EMBED_CHUNK, POOL_NONE, POOL_MEAN,  # noqa: F401,E402
                      POOL_LAST, POOL_CLS, POOL_WMEAN, POOL_MAX, EPI_F16, EPI_F32, EPI_RESID_F32, EPI_SWIGLU, CLASSES,
-                     ROPE_PAIRS, ROPE_HALVES, ROPE_LINEAR, ROPE_BY_PARTS)
+                     ROPE_PAIRS, ROPE_HALVES, ROPE_LINEAR, ROPE_BY_PARTS, LOGPROBS_MAX_K, DTYPE_F32, DTYPE_F16)
 
 
 class HbError(RuntimeError):
@@ -105,6 +105,7 @@ _sig = {
     "hb_kv8_attention_workspace": [C.POINTER(ModelCfg), C.POINTER(RowsStruct), C.POINTER(C.c_size_t)],
     "hb_kv8_attention": [_P, _P, C.c_int32, C.POINTER(RowsStruct), _P, C.c_int64, _P, C.c_int64, C.c_float, _P,
                          C.c_size_t, _P],
+    "hb_logprobs": [_P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int64, _P, C.c_int32, _P, _P, _P, _P, _P],
     "hb_rope_table": [C.c_int32, C.c_int32, C.c_double, C.POINTER(RopeScaling), _P, _P],
     "hb_pool_arena_bytes": [C.POINTER(ModelCfg), C.c_int32, C.POINTER(C.c_size_t)],
     "hb_pool_create": [C.POINTER(ModelCfg), _P, C.c_size_t, C.c_int32, C.POINTER(_P)],
@@ -651,6 +652,28 @@ class Context:
     def argmax(self, logits, n_rows, out_tokens, stream=None):
         check(lib.hb_argmax(self.handle, C.c_void_p(logits.data_ptr()), n_rows,
                             C.c_void_p(out_tokens.data_ptr()), _stream_ptr(stream)), "hb_argmax")
+
+    def logprobs(self, logits, tokens, out_logprob, out_entropy=None, out_top_ids=None, out_top_logprobs=None, stream=None):
+        """hb_logprobs: logits fp32 or fp16 [n, vocab] (rows may be strided), tokens int32 [n] (negative = none),
+        out_logprob fp32 [n] (tokens and out_logprob both or neither None), out_entropy fp32 [n], and the
+        k = out_top_ids.shape[1] best alternatives: out_top_ids int32 [n, k], out_top_logprobs fp32 [n, k]."""
+        if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.float16) or (logits.numel() and logits.stride(1) != 1):
+            raise ValueError("logits: fp32 or fp16 [n, vocab] with unit column stride")
+        n, vocab = logits.shape
+        k = out_top_ids.shape[1] if out_top_ids is not None else 0
+        ptrs = []
+        for t, dt, shape, name in ((tokens, torch.int32, (n,), "tokens"), (out_logprob, torch.float32, (n,), "out_logprob"),
+                                   (out_entropy, torch.float32, (n,), "out_entropy"),
+                                   (out_top_ids, torch.int32, (n, k), "out_top_ids"),
+                                   (out_top_logprobs, torch.float32, (n, k), "out_top_logprobs")):
+            if t is not None and (t.dtype != dt or t.shape != shape or t.device != self.device or not t.is_contiguous()):
+                raise ValueError(f"{name}: a contiguous {dt} tensor {list(shape)} on {self.device}")
+            ptrs.append(t.data_ptr() if t is not None else None)
+        if logits.device != self.device:
+            raise ValueError(f"logits: on {self.device}")
+        stride = logits.stride(0) if n > 1 else max(logits.stride(0), vocab)
+        check(lib.hb_logprobs(self.handle, logits.data_ptr(), DTYPE_F32 if logits.dtype == torch.float32 else DTYPE_F16, n, vocab,
+                              stride, ptrs[0], k, ptrs[1], ptrs[2], ptrs[3], ptrs[4], _stream_ptr(stream)), "hb_logprobs")
 
     def gemm_pair(self, A, B, A2, B2, Cout, M, N, K, K2, epilogue, stream=None):
         check(lib.hb_gemm_pair(self.handle, C.c_void_p(A.data_ptr()), C.c_void_p(B.data_ptr()),
