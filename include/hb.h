@@ -303,9 +303,9 @@ HB_API int hb_argmax(hb_ctx* ctx, const float* logits, int32_t n_rows, int32_t* 
 
 /* Read (and clear) the device status word; synchronises `stream`.  0 = clean.
  * Non-zero: *out_code holds the OR of the bits below and the call returns
- * HB_ERR_DEVICE_STATUS.  Bits 0-5 mean a kernel gave up (a bounded wait expired,
- * an index check failed: outputs of that step are not valid); bit 6 is a value
- * report: the step ran, but an activation did not fit fp16. */
+ * HB_ERR_DEVICE_STATUS.  Bits 0-5, 7 and 8 mean a kernel gave up (a bounded wait
+ * expired, an index check failed: outputs of that step are not valid); bit 6 is a
+ * value report: the step ran, but an activation did not fit fp16. */
 enum {
   HB_STATUS_GEMM_WAIT = 1,        /* projection GEMM: a pipeline wait expired                 */
   HB_STATUS_ATTN_INDEX = 2,       /* attention: page id out of range                          */
@@ -314,6 +314,7 @@ enum {
   HB_STATUS_ATTN_WAIT = 16,       /* attention: a pipeline wait expired                       */
   HB_STATUS_SELFTEST_WAIT = 32,   /* hb_selftest_wait_expiry                                  */
   HB_STATUS_TOKEN_INDEX = 128,    /* hb_logprobs: a token id beyond the vocabulary (its row got NaN) */
+  HB_STATUS_LOGPROBS_WAIT = 256,  /* hb_logprobs: a pipeline wait expired                 */
   HB_STATUS_F16_RANGE = 64        /* a normed row or a SwiGLU output was NaN or beyond +-65504:
                                      finite values were stored saturated, NaN was stored as NaN */
 };

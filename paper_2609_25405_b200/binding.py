@@ -159,6 +159,12 @@ def _stream_ptr(stream):
     return C.c_void_p(stream.cuda_stream)
 
 
+def _stream_of(stream, device_index):
+    """Raw handle of `stream`, or of the device's current stream: without building a Stream object, which
+    costs as much as a small kernel's launch."""
+    return torch._C._cuda_getCurrentRawStream(device_index) if stream is None else stream.cuda_stream
+
+
 def bf16_from_f32(a, device="cuda"):
     """numpy float32 (bf16-exact values) -> torch bf16 tensor on `device`, bit-exact."""
     bits = (np.ascontiguousarray(a, dtype=np.float32).view(np.uint32) >> np.uint32(16)).astype(np.uint16)
@@ -456,6 +462,7 @@ class KvCache8(KvCache):
                 self.arena = torch.empty(nbytes, dtype=torch.uint8, device=device)
             if fill is not None:
                 self.arena.fill_(fill)
+        self.device = self.arena.device if self.arena is not None else None
         ptr = C.c_void_p(self.arena.data_ptr()) if self.arena is not None else None
         check(lib.hb_kv8_create(C.byref(cfg), ptr, nbytes, n_pages, C.byref(self.handle)), "hb_kv8_create")
 
@@ -502,8 +509,18 @@ class SegRows:
             raise ValueError("segs [R, 12], page_ids [n], row_seg [T]")
         self.segs, self.page_ids, self.row_seg = segs, page_ids, row_seg
         self.device = segs.device
+        self._need = {}            # workspace bytes by (n_kv_heads, head_dim)
         self.struct = RowsStruct(segs.data_ptr(), page_ids.data_ptr(), row_seg.data_ptr(), segs.shape[0],
                                  page_ids.shape[0], row_seg.shape[0], int(max_q_len), int(max_keys))
+
+    def workspace_bytes(self, cfg):
+        """hb_kv8_attention_workspace of these rows."""
+        key = (cfg.n_kv_heads, cfg.head_dim)
+        if key not in self._need:
+            need = C.c_size_t()
+            check(lib.hb_kv8_attention_workspace(C.byref(cfg), C.byref(self.struct), C.byref(need)), "hb_kv8_attention_workspace")
+            self._need[key] = need.value
+        return self._need[key]
 
     @classmethod
     def from_batch(cls, batch, device="cuda"):
@@ -542,10 +559,11 @@ def rope_table(n_pos, rot_dim, theta, scaling=None):
 
 def _rows_f16(t, rows, cols, device, name):
     """A [>= rows, cols] fp16 matrix with unit column stride: (pointer, row stride)."""
-    if t.dtype != torch.float16 or t.device != device or t.dim() != 2 or t.shape[0] < rows or t.shape[1] != cols or \
-            (t.numel() and t.stride(1) != 1):
+    if t.dtype is not torch.float16 or t.device != device or t.dim() != 2 or t.size(0) < rows or t.size(1) != cols or \
+            (t.stride(1) != 1 and rows > 0):
         raise ValueError(f"{name}: an fp16 tensor [{rows}, {cols}] with unit column stride on {device}")
-    return C.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), cols))
+    stride = t.stride(0)
+    return t.data_ptr(), (stride if rows > 1 or stride >= cols else cols)
 
 
 class Pool:
@@ -657,23 +675,32 @@ class Context:
         """hb_logprobs: logits fp32 or fp16 [n, vocab] (rows may be strided), tokens int32 [n] (negative = none),
         out_logprob fp32 [n] (tokens and out_logprob both or neither None), out_entropy fp32 [n], and the
         k = out_top_ids.shape[1] best alternatives: out_top_ids int32 [n, k], out_top_logprobs fp32 [n, k]."""
-        if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.float16) or (logits.numel() and logits.stride(1) != 1):
-            raise ValueError("logits: fp32 or fp16 [n, vocab] with unit column stride")
-        n, vocab = logits.shape
-        k = out_top_ids.shape[1] if out_top_ids is not None else 0
-        ptrs = []
-        for t, dt, shape, name in ((tokens, torch.int32, (n,), "tokens"), (out_logprob, torch.float32, (n,), "out_logprob"),
-                                   (out_entropy, torch.float32, (n,), "out_entropy"),
-                                   (out_top_ids, torch.int32, (n, k), "out_top_ids"),
-                                   (out_top_logprobs, torch.float32, (n, k), "out_top_logprobs")):
-            if t is not None and (t.dtype != dt or t.shape != shape or t.device != self.device or not t.is_contiguous()):
-                raise ValueError(f"{name}: a contiguous {dt} tensor {list(shape)} on {self.device}")
-            ptrs.append(t.data_ptr() if t is not None else None)
-        if logits.device != self.device:
-            raise ValueError(f"logits: on {self.device}")
-        stride = logits.stride(0) if n > 1 else max(logits.stride(0), vocab)
-        check(lib.hb_logprobs(self.handle, logits.data_ptr(), DTYPE_F32 if logits.dtype == torch.float32 else DTYPE_F16, n, vocab,
-                              stride, ptrs[0], k, ptrs[1], ptrs[2], ptrs[3], ptrs[4], _stream_ptr(stream)), "hb_logprobs")
+        dev, dt = self.device, logits.dtype
+        if logits.dim() != 2 or (dt is not torch.float32 and dt is not torch.float16) or logits.device != dev or \
+                (logits.stride(1) != 1 and logits.numel()):
+            raise ValueError(f"logits: fp32 or fp16 [n, vocab] with unit column stride on {dev}")
+        n, vocab = logits.size(0), logits.size(1)
+        k = 0 if out_top_ids is None else out_top_ids.size(-1)
+        tp = self._vector(tokens, torch.int32, n, 1, "tokens")
+        lp = self._vector(out_logprob, torch.float32, n, 1, "out_logprob")
+        ep = self._vector(out_entropy, torch.float32, n, 1, "out_entropy")
+        ip = self._vector(out_top_ids, torch.int32, n, k, "out_top_ids")
+        vp = self._vector(out_top_logprobs, torch.float32, n, k, "out_top_logprobs")
+        stride = logits.stride(0)
+        if n <= 1 and stride < vocab:
+            stride = vocab
+        rc = lib.hb_logprobs(self.handle, logits.data_ptr(), DTYPE_F32 if dt is torch.float32 else DTYPE_F16, n, vocab, stride, tp,
+                             k, lp, ep, ip, vp, _stream_of(stream, dev.index))
+        if rc != HB_OK:
+            raise HbError(rc, "hb_logprobs")
+
+    def _vector(self, t, dtype, n, k, name):
+        """Pointer of a contiguous [n] (k = 1) or [n, k] tensor, or None."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.device != self.device or t.dim() > 2 or t.size(0) != n or t.numel() != n * k or not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous {dtype} tensor of {n} x {k} on {self.device}")
+        return t.data_ptr()
 
     def gemm_pair(self, A, B, A2, B2, Cout, M, N, K, K2, epilogue, stream=None):
         check(lib.hb_gemm_pair(self.handle, C.c_void_p(A.data_ptr()), C.c_void_p(B.data_ptr()),
@@ -694,7 +721,7 @@ class Context:
     def _same_device(self, rows, kv):
         if not isinstance(kv, KvCache8):
             raise TypeError("an 8-bit cache (KvCache8)")
-        if rows.device != self.device or kv.arena is None or kv.arena.device != self.device:
+        if rows.device != self.device or kv.device != self.device:
             raise ValueError(f"rows and cache on the context's device, {self.device}")
         return self.device
 
@@ -719,8 +746,9 @@ class Context:
                 raise ValueError(f"rope: tables on {dev}")
             a.rope_cos, a.rope_sin = rope.cos.data_ptr(), rope.sin.data_ptr()
             a.rope_rows, a.rot_dim, a.rope_layout = rope.cos.shape[0], 2 * rope.cos.shape[1], rope.layout
-        check(lib.hb_kv8_append(self.handle, kv.handle, layer, C.byref(rows.struct), C.byref(a), _stream_ptr(stream)),
-              "hb_kv8_append")
+        rc = lib.hb_kv8_append(self.handle, kv.handle, layer, C.byref(rows.struct), C.byref(a), _stream_of(stream, dev.index))
+        if rc != HB_OK:
+            raise HbError(rc, "hb_kv8_append")
 
     def kv8_attention(self, kv, layer, rows, q, out, scale=0.0, stream=None):
         """hb_kv8_attention: causal attention of every row of `rows` over its request's pages of layer `layer` of a
@@ -730,15 +758,18 @@ class Context:
         T, dev = rows.struct.n_rows, self._same_device(rows, kv)
         qp, qs = _rows_f16(q, T, c.n_heads * c.head_dim, dev, "q")
         op, os_ = _rows_f16(out, T, c.n_heads * c.head_dim, dev, "out")
-        need = C.c_size_t()
-        check(lib.hb_kv8_attention_workspace(C.byref(c), C.byref(rows.struct), C.byref(need)), "hb_kv8_attention_workspace")
-        ws = None
-        if need.value:   # allocated on the stream of the call, whose order then protects its reuse
-            with torch.cuda.stream(stream):
-                ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
-        check(lib.hb_kv8_attention(self.handle, kv.handle, layer, C.byref(rows.struct), qp, qs, op, os_, scale,
-                                   C.c_void_p(ws.data_ptr()) if ws is not None else None, need.value, _stream_ptr(stream)),
-              "hb_kv8_attention")
+        need, ws, wp = rows.workspace_bytes(c), None, None
+        if need:   # allocated on the stream of the call, whose order then protects its reuse
+            if stream is None:
+                ws = torch.empty(need, dtype=torch.uint8, device=dev)
+            else:
+                with torch.cuda.stream(stream):
+                    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+            wp = ws.data_ptr()
+        rc = lib.hb_kv8_attention(self.handle, kv.handle, layer, C.byref(rows.struct), qp, qs, op, os_, scale, wp, need,
+                                  _stream_of(stream, dev.index))
+        if rc != HB_OK:
+            raise HbError(rc, "hb_kv8_attention")
 
     def status_poll(self, stream=None):
         """Synchronises the stream; returns the device status code (0 = clean)."""

@@ -23,6 +23,7 @@ enum : uint32_t {
   HB_DEV_ATTN_WAIT_EXPIRED = 1u << 4,
   HB_DEV_SELFTEST_WAIT_EXPIRED = 1u << 5,
   HB_DEV_TOKEN_BAD_INDEX = 1u << 7,
+  HB_DEV_LOGPROBS_WAIT_EXPIRED = 1u << 8,
   HB_DEV_F16_RANGE = 1u << 6,   // a normed row or a SwiGLU output was NaN or beyond the largest finite half
 };
 
