@@ -2,13 +2,14 @@
 //
 //   s_ij = scale * q_i . k_j (j <= pos_i);  o_i = sum_j softmax(s_i)_j v_j
 //
-// Items.  The q_len * G rows a segment has for one KV head (G = Hq / Hkv; column c = row c / G, head c % G)
-// are cut into column tiles of 16; a segment of one tile (decode rows) has its keys cut into splits,
-// whose number depends on the segment's own length only.  Each block walks items b, b + grid, ...; the
-// segment of an item is found in a prefix sum over the segments that the block forms itself, so that
-// nothing about the batch has to be known on the host and a captured launch follows the arrays.
+// A segment has q_len * G columns for one KV head (G = Hq / Hkv; column c = row c / G, head c % G).  Segments of
+// up to 16 (decode rows) take the body in this file, their keys cut into splits whose number depends on
+// the segment's own length only; larger ones take the tcgen05 body of kv8_attention_tc.cuh in a launch
+// of its own.  Each block walks items b, b + grid, ...; the segment of an item is found in a prefix sum
+// over the segments that the block forms itself, so that nothing about the batch has to be known on the
+// host and a captured launch follows the arrays.
 //
-// One item: four warps share the columns and take every fourth page.  A warp fetches a page's block of
+// One decode item: four warps share the columns and take every fourth page.  A warp fetches a page's block of
 // this KV head (K, V and scales: 2 - 4 KiB, contiguous) with one bulk copy into its own ring and
 // computes transposed, so that the 16 keys of the page fill the 16 rows of the matrix instruction
 // whatever G is:
@@ -66,54 +67,54 @@ __device__ __forceinline__ bool load_seg(const Rows& r, int s, Seg& g) {
   return seg_ok(r, g.q_start, g.q_len, g.pos_start, g.pt_start, b.y);
 }
 
-// Items of a segment: column tiles x splits (only one-tile segments are split), times the KV heads.
-__device__ __forceinline__ int tiles_of(const Rows& r, const Seg& g) { return (g.q_len * r.G + TILE_COLS - 1) / TILE_COLS; }
-__device__ __forceinline__ int splits_of(int tiles, const Seg& g) { return tiles == 1 ? n_splits(g.pos_start + g.q_len) : 1; }
+// Splits of a segment of the decode body: one to 16 columns (0: no rows, or rows for the chunk body).
+__device__ __forceinline__ int splits_of(const Rows& r, const Seg& g) {
+  const int cols = g.q_len * r.G;
+  return cols < 1 || cols > TILE_COLS ? 0 : n_splits(g.pos_start + g.q_len);
+}
 
-struct Item {
-  Seg g;
-  int seg, head, tile, split, ns;
-  int col0, n_cols;   // columns of this tile
-  int key0, key1;     // keys [key0, key1) that some column of the tile may see
-};
-
-__device__ __forceinline__ void find_item(const AttnParams& p, const int* prefix, int idx, Item& it) {
-  int lo = 0, hi = p.r.n_segs;   // prefix[lo] <= idx < prefix[hi]
+// Segment that item idx belongs to: prefix[s] <= idx < prefix[s + 1].
+__device__ __forceinline__ int find_seg(const int* prefix, int n_segs, int idx) {
+  int lo = 0, hi = n_segs;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (prefix[mid] <= idx) lo = mid; else hi = mid;
   }
-  it.seg = lo;
-  load_seg(p.r, lo, it.g);
-  const int tiles = tiles_of(p.r, it.g), keys = it.g.pos_start + it.g.q_len;
-  it.ns = splits_of(tiles, it.g);
-  int at = idx - prefix[lo];
-  it.head = at % p.r.Hkv;
-  at /= p.r.Hkv;
-  it.split = at % it.ns;
-  it.tile = at / it.ns;
-  it.col0 = it.tile * TILE_COLS;
-  it.n_cols = min(TILE_COLS, it.g.q_len * p.r.G - it.col0);
-  const int seen = it.g.pos_start + (it.col0 + it.n_cols - 1) / p.r.G + 1;
-  const int per = it.ns > 1 ? split_keys(keys) : keys;
-  it.key0 = it.split * per;
-  it.key1 = min(seen, it.key0 + per);
+  return lo;
 }
 
-// prefix[s] = items before segment s; returns the total.  All threads; ends with a barrier.
-__device__ int build_prefix(const AttnParams& p, int* prefix, int* warp_sums) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.r.n_segs;
-  const int per = (n + DEC_THREADS - 1) / DEC_THREADS, from = min(n, tid * per), to = min(n, from + per);
+struct Item {
+  Seg g;
+  int seg, head, split, ns;
+  int n_cols;
+  int key0, key1;     // keys [key0, key1) of this split
+};
+
+__device__ __forceinline__ void find_item(const AttnParams& p, const int* prefix, int idx, Item& it) {
+  it.seg = find_seg(prefix, p.r.n_segs, idx);
+  load_seg(p.r, it.seg, it.g);
+  const int keys = it.g.pos_start + it.g.q_len, at = idx - prefix[it.seg];
+  it.ns = splits_of(p.r, it.g);
+  it.head = at % p.r.Hkv;
+  it.split = at / p.r.Hkv;
+  it.n_cols = it.g.q_len * p.r.G;
+  const int per = it.ns > 1 ? split_keys(keys) : keys;
+  it.key0 = it.split * per;
+  it.key1 = min(keys, it.key0 + per);
+}
+
+// prefix[s] = items before segment s (items(segment) each); returns the total.  All threads of the block; ends
+// with a barrier.
+template <int THREADS, class F>
+__device__ int build_prefix(const Rows& r, int* prefix, int* warp_sums, F&& items_of, bool report) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = r.n_segs;
+  const int per = (n + THREADS - 1) / THREADS, from = min(n, tid * per), to = min(n, from + per);
   int sum = 0;
   for (int s = from; s < to; ++s) {
     Seg g;
     int items = 0;
-    if (load_seg(p.r, s, g)) {
-      const int tiles = tiles_of(p.r, g);
-      items = tiles * splits_of(tiles, g) * p.r.Hkv;
-    } else if (blockIdx.x == 0) {
-      atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
-    }
+    if (load_seg(r, s, g)) items = items_of(g);
+    else if (report && blockIdx.x == 0) atomicOr(r.status, HB_DEV_ATTN_BAD_INDEX);
     prefix[s] = sum;
     sum += items;
   }
@@ -127,7 +128,7 @@ __device__ int build_prefix(const AttnParams& p, int* prefix, int* warp_sums) {
   __syncthreads();
   int base = incl - sum, total = 0;
 #pragma unroll
-  for (int w = 0; w < DEC_WARPS; ++w) {
+  for (int w = 0; w < THREADS / 32; ++w) {
     if (w < warp) base += warp_sums[w];
     total += warp_sums[w];
   }
@@ -136,6 +137,12 @@ __device__ int build_prefix(const AttnParams& p, int* prefix, int* warp_sums) {
   __syncthreads();
   return total;
 }
+
+}  // namespace
+
+#include "kv8_attention_tc.cuh"
+
+namespace {
 
 template <int DH>
 struct DecCfg {
@@ -169,7 +176,7 @@ __device__ __forceinline__ void begin(const AttnParams& p, const Item& it, State
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int c = nt * 8 + g;
-    const int col = it.col0 + min(c, it.n_cols - 1);
+    const int col = min(c, it.n_cols - 1);
     const __half* src = p.q + (it.g.q_start + col / p.r.G) * p.q_stride + (it.head * p.r.G + col % p.r.G) * DH + t * 16;
 #pragma unroll
     for (int hf = 0; hf < DH / 64; ++hf) {
@@ -190,7 +197,7 @@ __device__ __forceinline__ void begin(const AttnParams& p, const Item& it, State
       const int cc = nt * 8 + 2 * t + e;
       st.m[nt][e] = -INFINITY;
       st.l[nt][e] = 0.0f;
-      st.lim[nt][e] = cc < it.n_cols ? min(it.key1 - 1, it.g.pos_start + (it.col0 + cc) / p.r.G) : -1;
+      st.lim[nt][e] = cc < it.n_cols ? min(it.key1 - 1, it.g.pos_start + cc / p.r.G) : -1;
     }
   }
 }
@@ -398,8 +405,7 @@ __device__ __forceinline__ bool run_item(const AttnParams& p, const Item& it, Ri
         }
         if (it.ns == 1) {
           const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-          const int col = it.col0 + c;
-          __half* dst = p.out + (it.g.q_start + col / p.r.G) * p.out_stride + (it.head * p.r.G + col % p.r.G) * DH + d;
+          __half* dst = p.out + (it.g.q_start + c / p.r.G) * p.out_stride + (it.head * p.r.G + c % p.r.G) * DH + d;
           *reinterpret_cast<uint32_t*>(dst) = pack_half2_sat(x * inv, y * inv);
         } else {
           const int64_t rec = (static_cast<int64_t>(it.seg) * p.r.Hkv + it.head) * p.max_splits + it.split;
@@ -431,7 +437,7 @@ kv8_attend_kernel(const AttnParams p) {
   if (tid < DEC_WARPS * STAGES) mbar_init(smem_u32(tail) + 8u * tid, 1);
   if (tid == 0) *abort_flag = 0u;
   mbar_init_fence();
-  const int total = build_prefix(p, prefix, warp_sums);   // its barriers publish the initialisation
+  const int total = build_prefix<DEC_THREADS>(p.r, prefix, warp_sums, [&](const Seg& g) { return splits_of(p.r, g) * p.r.Hkv; }, true);   // its barriers publish the initialisation
   for (int idx = blockIdx.x; idx < total; idx += gridDim.x) {
     Item it;
     find_item(p, prefix, idx, it);
@@ -458,8 +464,8 @@ kv8_join_kernel(const AttnParams p, const int cols) {
   const int c = blockIdx.x % cols, head = (blockIdx.x / cols) % p.r.Hkv, seg = blockIdx.x / (cols * p.r.Hkv);
   Seg g;
   if (!load_seg(p.r, seg, g)) return;
-  const int tiles = tiles_of(p.r, g), ns = splits_of(tiles, g);
-  if (tiles != 1 || ns == 1 || c >= g.q_len * p.r.G) return;
+  const int ns = splits_of(p.r, g);
+  if (ns <= 1 || c >= g.q_len * p.r.G) return;
   const int64_t rec = (static_cast<int64_t>(seg) * p.r.Hkv + head) * p.max_splits;
   float m = -INFINITY;
   for (int s = 0; s < ns; ++s) {
@@ -488,12 +494,20 @@ int launch(const AttnParams& p, int num_sms, cudaStream_t s, bool pdl) {
   auto kern = kv8_attend_kernel<DH>;
   if (hb_ensure_dyn_smem(reinterpret_cast<const void*>(kern), configured, smem) != HB_OK) return HB_ERR_CUDA;
   // no more blocks than the bounds of the call allow items
-  const long long tiles = (static_cast<long long>(p.r.max_q_len) * p.r.G + TILE_COLS - 1) / TILE_COLS;
-  const long long most = static_cast<long long>(p.r.n_segs) * p.r.Hkv * std::max<long long>(tiles, p.max_splits);
-  const int blocks = static_cast<int>(std::min<long long>(most, 3ll * num_sms));
-  int rc = hb_launch_kernel(kern, blocks, DEC_THREADS, smem, s, pdl, p);
+  const long long most = static_cast<long long>(p.r.n_segs) * p.r.Hkv * p.max_splits;
+  int rc = hb_launch_kernel(kern, static_cast<unsigned>(std::min<long long>(most, 3ll * num_sms)), DEC_THREADS, smem, s, pdl, p);
+  const long long cols_bound = static_cast<long long>(p.r.max_q_len) * p.r.G;
+  if (rc == HB_OK && cols_bound > TILE_COLS) {   // segments for the chunk body are possible
+    static DynSmemState tc_configured;
+    const int tc_smem = hb_kv8_tc::Cfg<DH>::FIXED + (p.r.n_segs + 1) * 4;
+    if (tc_smem > 227 * 1024) return HB_ERR_TOO_LARGE;
+    auto tc = hb_kv8_tc::kv8_chunk_kernel<DH>;
+    if (hb_ensure_dyn_smem(reinterpret_cast<const void*>(tc), tc_configured, tc_smem) != HB_OK) return HB_ERR_CUDA;
+    const long long tc_most = static_cast<long long>(p.r.n_segs) * p.r.Hkv * ((cols_bound + hb_kv8_tc::ROWS - 1) / hb_kv8_tc::ROWS);
+    rc = hb_launch_kernel(tc, static_cast<unsigned>(std::min<long long>(tc_most, num_sms)), hb_kv8_tc::THREADS, tc_smem, s, true, p);
+  }
   if (rc != HB_OK || p.max_splits == 1) return rc;
-  const int cols = static_cast<int>(std::min<long long>(TILE_COLS, static_cast<long long>(p.r.max_q_len) * p.r.G));
+  const int cols = static_cast<int>(std::min<long long>(TILE_COLS, cols_bound));
   return hb_launch_kernel(kv8_join_kernel<DH>, static_cast<unsigned>(p.r.n_segs) * p.r.Hkv * cols, DH, 0, s, true, p, cols);
 }
 

@@ -155,7 +155,8 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int k, ui
   }
 }
 
-template <typename T, bool ALIGNED>
+// TOP: alternatives are asked for (p.k > 0); scoring alone does without the code that looks for them.
+template <typename T, bool ALIGNED, bool TOP>
 __global__ void __launch_bounds__(THREADS, 3)
 logprobs_kernel(const Params p) {
   using H = Shape<T>;
@@ -222,6 +223,12 @@ logprobs_kernel(const Params p) {
     int cur = 0, have = 0, part = part0, c0 = first_of(part0), to = first_of(part0 + 1);
     for (bool more = true; more;) {
       const int held = min(CHUNKS, to - c0);   // (a part behind the last chunk has none)
+      const bool part_ends = c0 + CHUNKS >= to, row_ends = part_ends && part + 1 == part1;
+      const int next_part = part_ends ? part + 1 : part, next_c0 = part_ends ? first_of(part + 1) : c0 + CHUNKS;
+      auto ask_next = [&]() {
+        if (!row_ends) request(row, next_c0, first_of(next_part + 1));
+        else if (row + n_clusters < p.n_rows) request(row + n_clusters, first_of(part0), first_of(part0 + 1));
+      };
       complete(logits, c0, to);
       // ---- the slice's maximum ----
       float mx = -INFINITY;
@@ -237,7 +244,7 @@ logprobs_kernel(const Params p) {
       {
         const float w = warp_max(mx);
         if (lane == 0) warp_val[warp] = w;
-        if (p.k > 0) {
+        if (TOP) {
           float g = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
           g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
           if ((tid & 3) == 0) group_max[tid >> 2] = order(g);
@@ -249,7 +256,16 @@ logprobs_kernel(const Params p) {
 #pragma unroll
       for (int w = 1; w < WARPS; ++w) M = fmaxf(M, warp_val[w]);
       const float ref = M == -INFINITY ? 0.0f : M;
-      if (p.k > 0) {   // k-th largest group maximum, equal ones by group
+      // Only logits that reach `low` (and then keys above `floor_key`) can be alternatives: the k-th best so far,
+      // or, while there are fewer, the k-th largest group maximum (equal ones by group).
+      const bool listed = TOP && have == p.k;
+      uint64_t floor_key = 0;
+      float low = INFINITY;
+      if (TOP && listed) {
+        floor_key = lists[cur][p.k - 1];
+        low = key_value(floor_key);
+        if (low != low) low = -INFINITY;   // (NaN is among them)
+      } else if (TOP) {
         const uint64_t mine = group_max[tid >> 2];
         int above = 0;
 #pragma unroll
@@ -260,8 +276,20 @@ logprobs_kernel(const Params p) {
         above += __shfl_xor_sync(0xffffffffu, above, 1);
         above += __shfl_xor_sync(0xffffffffu, above, 2);
         if ((tid & 3) == 0 && above == p.k - 1) val_bound = key_value(mine << 32);
+        __syncthreads();
+        low = val_bound;
       }
-      // ---- the sums ----
+      auto keep = [&](float x, int idx, uint64_t bound) {
+        if (idx < p.vocab) {
+          const uint64_t key = make_key(x, idx);
+          if (key > bound) {
+            const int place = atomicAdd(&n_cand, 1);
+            if (place < CAP - MAX_K) cand[place] = key;
+          }
+        }
+      };
+      // ---- the sums, and the logits that reach the bound ----
+      const bool reaches = TOP && mx >= low;
       float s, q;
       {
         // two logits per instruction.  Below -200 the exponential is zero; the clamp keeps -inf out of the
@@ -273,7 +301,13 @@ logprobs_kernel(const Params p) {
 #pragma unroll
           for (int v = 0; v < VECS; ++v) {
             float x[V];
-            widen<T>(vec[v * THREADS], x);
+            const uint4 raw = vec[v * THREADS];
+            widen<T>(raw, x);
+            if (reaches && vector_max<T>(raw) >= low) {
+#pragma unroll
+              for (int e = 0; e < V; ++e)
+                if (x[e] >= low) keep(x[e], (c0 + c) * H::PER_CHUNK + (v * THREADS + tid) * V + e, floor_key);
+            }
 #pragma unroll
             for (int e = 0; e < V; e += 2) {
               float a, b;
@@ -301,7 +335,9 @@ logprobs_kernel(const Params p) {
         if (lane == 0) warp_s[warp] = v;
         if (lane == 16) warp_q[warp] = v;
       }
+      fence_async_smem();   // this slice's accesses to shared memory, before copies into it
       __syncthreads();
+      int n = n_cand;
       s = warp_s[0];
       q = warp_q[0];
 #pragma unroll
@@ -309,8 +345,10 @@ logprobs_kernel(const Params p) {
       // One of the maxima is the 1 of 1 + T.  While the rest is not small against it, it can be taken off
       // the sum; else the sum is formed again without the maxima, which are counted.
       float T_ = M == -INFINITY ? s : s - 1.0f;
+      bool reread = false;   // the slice was read after the last barrier
       if (M > -INFINITY && T_ < 0.25f) {
-        float n = 0.0f, small = 0.0f;
+        reread = true;
+        float tops = 0.0f, small = 0.0f;
         for (int c = 0; c < held; ++c) {
           const uint4* vec = reinterpret_cast<const uint4*>(smem + c * CHUNK) + tid;
           for (int v = 0; v < VECS; ++v) {
@@ -319,7 +357,7 @@ logprobs_kernel(const Params p) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
               const float d = max_nan(x[e] - ref, -200.0f);
-              n += d == 0.0f ? 1.0f : 0.0f;
+              tops += d == 0.0f ? 1.0f : 0.0f;
               small += d == 0.0f ? 0.0f : ex2_approx(d * LOG2E);
             }
           }
@@ -327,46 +365,19 @@ logprobs_kernel(const Params p) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
           small += __shfl_xor_sync(0xffffffffu, small, o);
-          n += __shfl_xor_sync(0xffffffffu, n, o);
+          tops += __shfl_xor_sync(0xffffffffu, tops, o);
         }
         __syncthreads();
-        if (lane == 0) { warp_s[warp] = small; warp_val[warp] = n; }
+        if (lane == 0) { warp_s[warp] = small; warp_val[warp] = tops; }
         __syncthreads();
         T_ = 0.0f;
-        n = -1.0f;
-        for (int w = 0; w < WARPS; ++w) { T_ += warp_s[w]; n += warp_val[w]; }
-        T_ += n;
+        tops = -1.0f;
+        for (int w = 0; w < WARPS; ++w) { T_ += warp_s[w]; tops += warp_val[w]; }
+        T_ += tops;
       }
       rec = join(rec, Rec{M, T_, q});
       // ---- alternatives ----
-      if (p.k > 0) {
-        // logits of this thread that reach `bound_val` and whose key reaches `bound_key`
-        auto collect = [&](float bound_val, uint64_t bound_key) {
-          if (mx >= bound_val) {
-            for (int c = 0; c < held; ++c) {
-              const uint4* vec = reinterpret_cast<const uint4*>(smem + c * CHUNK) + tid;
-#pragma unroll
-              for (int v = 0; v < VECS; ++v) {
-                const uint4 raw = vec[v * THREADS];
-                if (vector_max<T>(raw) >= bound_val) {
-                  float x[V];
-                  widen<T>(raw, x);
-#pragma unroll
-                  for (int e = 0; e < V; ++e) {
-                    const int idx = (c0 + c) * H::PER_CHUNK + (v * THREADS + tid) * V + e;
-                    if (x[e] >= bound_val && idx < p.vocab) {
-                      const uint64_t key = make_key(x[e], idx);
-                      if (key >= bound_key) {
-                        const int place = atomicAdd(&n_cand, 1);
-                        if (place < CAP - MAX_K) cand[place] = key;
-                      }
-                    }
-                  }
-                }
-              }
-            }
-          }
-        };
+      if (TOP) {
         // largest key of this thread that is below `limit` (0: none)
         auto best_below = [&](uint64_t limit) {
           uint64_t best = 0;
@@ -383,14 +394,11 @@ logprobs_kernel(const Params p) {
             }
           return best;
         };
-        const float low = val_bound;
-        collect(low, 0);
-        __syncthreads();
-        int n = n_cand;
         if (n > CAP - MAX_K) {
-          // too many reach it: the same bound over keys, which are all different
+          reread = true;
+          // too many reach it: a bound over keys, which are all different
           __syncthreads();
-          uint64_t best = mx >= low ? best_below(~0ull) : 0ull;
+          uint64_t best = reaches ? best_below(~0ull) : 0ull;
           best = max(best, __shfl_xor_sync(0xffffffffu, best, 1));
           best = max(best, __shfl_xor_sync(0xffffffffu, best, 2));
           if ((tid & 3) == 0) group_max[tid >> 2] = best;
@@ -401,15 +409,25 @@ logprobs_kernel(const Params p) {
           for (int g = tid & 3; g < GROUPS; g += 4) above += group_max[g] > mine;
           above += __shfl_xor_sync(0xffffffffu, above, 1);
           above += __shfl_xor_sync(0xffffffffu, above, 2);
-          if ((tid & 3) == 0 && mine != 0 && above == p.k - 1) key_bound = mine;
+          if ((tid & 3) == 0 && mine != 0 && above == p.k - 1) key_bound = mine - 1;
           __syncthreads();
-          collect(low, key_bound);
+          const uint64_t bound = max(floor_key, key_bound);
+          if (reaches)
+            for (int c = 0; c < held; ++c)
+              for (int v = 0; v < VECS; ++v) {
+                float x[V];
+                widen<T>(reinterpret_cast<const uint4*>(smem + c * CHUNK)[v * THREADS + tid], x);
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                  if (x[e] >= low) keep(x[e], (c0 + c) * H::PER_CHUNK + (v * THREADS + tid) * V + e, bound);
+              }
           __syncthreads();
           n = n_cand;
         }
-        const int there = min(to * H::PER_CHUNK, p.vocab) - c0 * H::PER_CHUNK;   // logits of this and later chunks (or fewer than k)
-        if (n > CAP - MAX_K || n < min(p.k, min(there, held * H::PER_CHUNK))) {
+        const int there = min(min(to * H::PER_CHUNK, p.vocab) - c0 * H::PER_CHUNK, held * H::PER_CHUNK);   // logits of this slice
+        if (n > CAP - MAX_K || (!listed && n < min(p.k, there))) {
           // one by one
+          reread = true;
           uint64_t limit = ~0ull;
           int found = 0;
           for (; found < p.k; ++found) {
@@ -426,18 +444,23 @@ logprobs_kernel(const Params p) {
           }
           n = found;
         }
-        // rank what was collected and what earlier chunks left
+      }
+      if (reread) {
+        fence_async_smem();
+        __syncthreads();
+      }
+      ask_next();   // nobody needs the slice any more
+      if (TOP && n > 0) {
+        // rank what was collected and what earlier slices left
         if (tid < have) cand[n + tid] = lists[cur][tid];
         if (tid < MAX_K) lists[cur ^ 1][tid] = 0;
         __syncthreads();
         rank_keys(cand, n + have, p.k, lists[cur ^ 1]);
         cur ^= 1;
         have = min(p.k, n + have);
+        __syncthreads();
       }
-      fence_async_smem();   // this slice's accesses to shared memory, before copies into it
-      __syncthreads();
-      c0 += CHUNKS;
-      if (c0 >= to) {   // the part is done: its record goes to rank 0
+      if (part_ends) {   // its record goes to rank 0
         if (tid == 0) {
           const uint32_t rec_to = map_to_rank(smem_u32(&recs[buf][part]), 0);
           st_cluster_u32(rec_to, __float_as_uint(rec.m));
@@ -445,14 +468,12 @@ logprobs_kernel(const Params p) {
           st_cluster_u32(rec_to + 8, __float_as_uint(rec.S));
         }
         rec = Rec{-INFINITY, 0.0f, 0.0f};
-        ++part;
-        more = part < part1;
-        c0 = first_of(part);
-        to = first_of(part + 1);
       }
-      if (more) request(row, c0, to);
+      more = !row_ends;
+      part = next_part;
+      c0 = next_c0;
+      to = first_of(part + 1);
     }
-    if (row + n_clusters < p.n_rows) request(row + n_clusters, first_of(part0), first_of(part0 + 1));
     // ---- rank 0 joins the parts ----
     if (size > 1) {
       const uint32_t list_to = map_to_rank(smem_u32(&gathered[buf][rank * p.k]), 0);
@@ -469,7 +490,7 @@ logprobs_kernel(const Params p) {
     rec = recs[buf][0];
     for (int v = 1; v < p.parts; ++v) rec = join(rec, recs[buf][v]);
     if (size > 1) {
-      if (p.k > 0) {
+      if (TOP) {
         rank_keys(gathered[buf], static_cast<int>(size) * p.k, p.k, lists[cur]);
         __syncthreads();
       }
@@ -517,9 +538,9 @@ int launch(Params p, int num_sms, cudaStream_t s) {
   cfg.gridDim = dim3(static_cast<unsigned>(clusters) * size);
   cfg.blockDim = dim3(THREADS);
   const int smem = CHUNKS * CHUNK;
-  static DynSmemState configured;
-  auto kern = logprobs_kernel<T, ALIGNED>;
-  if (hb_ensure_dyn_smem(reinterpret_cast<const void*>(kern), configured, smem) != HB_OK) return HB_ERR_CUDA;
+  static DynSmemState configured[2];
+  auto kern = p.k > 0 ? logprobs_kernel<T, ALIGNED, true> : logprobs_kernel<T, ALIGNED, false>;
+  if (hb_ensure_dyn_smem(reinterpret_cast<const void*>(kern), configured[p.k > 0], smem) != HB_OK) return HB_ERR_CUDA;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];

@@ -226,6 +226,20 @@ def test_chunks(hq, hkv, dh):
     print("\n  worst error / bound:", _check_attend(ctx, kv, 0, rows, hq, hkv, dh, 12))
 
 
+@pytest.mark.parametrize("hq,hkv,dh", [(32, 8, 128), (32, 8, 64), (8, 8, 128), (16, 1, 64)])
+def test_many_chunks(hq, hkv, dh):
+    """More items than SMs, so that every resident block of the chunk body walks through several: blocks of 256 rows with one
+    and with two row tiles, key ranges of every length, one after the other."""
+    cfg, ctx = context(hq, hkv, dh)
+    r = np.random.default_rng(hq + dh)
+    segs = [(int(r.integers(0, 600)), int(q)) for q in r.integers(17, 400, 40 if hkv == 1 else 14)]
+    n_pages = sum((p + q + 15) // 16 for p, q in segs)
+    kv = random_arena(cfg, n_pages, seed=dh + 1)
+    rows = Rows(segs, n_pages, seed=hq)
+    items = sum((q * (hq // hkv) + 255) // 256 for _, q in segs) * hkv
+    print("\n ", items, "items, worst error / bound:", _check_attend(ctx, kv, 0, rows, hq, hkv, dh, 12))
+
+
 @pytest.mark.parametrize("scale_lo,scale_hi", [(-32, -30), (-14, 10), (0, 0)])
 def test_block_scales_far_apart(scale_lo, scale_hi):
     """Scales of neighbouring pages that differ by up to 2^24 (K's are kept small so that the scores stay finite)."""
