@@ -552,7 +552,8 @@ HB_API int hb_kv8_append(hb_ctx* ctx, hb_kv* kv, int32_t layer, const hb_rows* r
  *        initialisation and belongs to the call until it has run: calls that may run at the same
  *        time need a workspace each
  * Scores, softmax and sums in fp32, probabilities rounded to fp16 for the tensor cores.  How a
- * segment's keys are split depends on its own lengths only, never on the rest of the batch. */
+ * segment's keys are split depends on its own lengths only, never on the rest of the batch.  (Inside
+ * hb_mixed_step the splits may be longer: there the context's limits choose them.) */
 HB_API int hb_kv8_attention_workspace(const hb_model_cfg* cfg, const hb_rows* rows, size_t* out_bytes);
 HB_API int hb_kv8_attention(hb_ctx* ctx, hb_kv* kv, int32_t layer, const hb_rows* rows, const void* q, int64_t q_stride,
                      void* out, int64_t out_stride, float scale, void* workspace, size_t workspace_bytes, void* stream);

@@ -220,9 +220,11 @@ int hb_launch_bf16_to_f16(const void* src, void* dst, size_t n, cudaStream_t s);
 // 8-bit KV cache (kv8_append.cu, kv8_attention.cu)
 namespace hb_kv8 { struct Rows; }
 int hb_launch_kv8_append(hb_ctx* c, const hb_kv8::Rows& r, const hb_append_args& a, cudaStream_t s, bool pdl);
+// min_split: keys per split of a decode row; *launches: kernels launched
 int hb_launch_kv8_attention(hb_ctx* c, const hb_kv8::Rows& r, const void* q, int64_t q_stride, void* out, int64_t out_stride,
-                            float scale, void* workspace, cudaStream_t s, bool pdl);
-size_t hb_kv8_attention_scratch(int n_segs, int n_kv_heads, int head_dim, int max_keys);   // bytes of workspace
+                            float scale, int min_split, void* workspace, cudaStream_t s, bool pdl, int* launches);
+size_t hb_kv8_attention_scratch(const hb_model_cfg& cfg, int n_rows, int n_segs, int max_keys, int min_split);   // bytes of workspace
+int hb_kv8_min_split_keys();
 int hb_kv8_max_segs();
 
 struct hb_ctx {

@@ -58,6 +58,7 @@ struct Layout {
   size_t total, desc_cap, attn_part_floats, pool_part_floats;
   int32_t rows_pad, logit_rows_pad, n_counters, max_pool_items, max_attn_items, n_resid_turns;
   int32_t split_keys;   // keys per decode attention item of this context
+  int32_t kv8_split_keys;   // the same over an 8-bit cache
 };
 
 Layout make_layout(const hb_model_cfg& c, int32_t max_tokens, int32_t max_segs, int32_t max_page_ids) {
@@ -72,7 +73,14 @@ Layout make_layout(const hb_model_cfg& c, int32_t max_tokens, int32_t max_segs, 
   L.h = cv.take(rows * c.d_model * 2);
   L.q = cv.take(rows * n_q * 2);
   L.attn_out = cv.take(rows * n_q * 2);
-  L.act = cv.take(rows * c.d_ffn * 2);
+  // act also holds what a step over an 8-bit cache needs between its QKV projection and its O projection: the
+  // projection's fp16 rows, then (appended) the records of the decode splits.  A split there is as short as
+  // the records of max_segs requests of max_pos tokens allow; the context's limits decide, not the batch.
+  const size_t n_qkv = n_q + 2ull * c.n_kv_heads * c.head_dim;
+  const size_t act_bytes = rows * std::max<size_t>(c.d_ffn, n_qkv) * 2;
+  L.act = cv.take(act_bytes);
+  L.kv8_split_keys = hb_kv8_min_split_keys();
+  while (hb_kv8_attention_scratch(c, max_tokens, max_segs, c.max_pos, L.kv8_split_keys) > act_bytes) L.kv8_split_keys *= 2;
   L.lora_u = cv.take(rows * HB_LORA_U_COLS * 2);
   L.lora_part = cv.take(static_cast<size_t>(HB_LORA_K_SPLITS) * rows * HB_LORA_U_COLS * 4);
   L.lora_counters = cv.take((rows / 128) * 2 * 8 * 4);
@@ -610,9 +618,9 @@ int hb_kv8_append(hb_ctx* c, hb_kv* kv, int32_t layer, const hb_rows* rows, cons
 }
 
 int hb_kv8_attention_workspace(const hb_model_cfg* cfg, const hb_rows* rows, size_t* out_bytes) {
-  if (!cfg_ok(cfg) || !rows || !out_bytes || rows->n_segs < 0 || rows->max_keys < 0) return HB_ERR_BAD_ARG;
+  if (!cfg_ok(cfg) || !rows || !out_bytes || rows->n_rows < 0 || rows->n_segs < 0 || rows->max_keys < 0) return HB_ERR_BAD_ARG;
   if (rows->n_segs > hb_kv8_max_segs()) return HB_ERR_TOO_LARGE;
-  *out_bytes = hb_kv8_attention_scratch(rows->n_segs, cfg->n_kv_heads, cfg->head_dim, rows->max_keys);
+  *out_bytes = hb_kv8_attention_scratch(*cfg, rows->n_rows, rows->n_segs, rows->max_keys, hb_kv8_min_split_keys());
   return HB_OK;
 }
 
@@ -625,12 +633,14 @@ int hb_kv8_attention(hb_ctx* c, hb_kv* kv, int32_t layer, const hb_rows* rows, c
   if (q_stride < n_q || q_stride % 8 || out_stride < n_q || out_stride % 8) return HB_ERR_BAD_ARG;
   if (misaligned(q, 16) || misaligned(out, 16)) return HB_ERR_BAD_ARG;
   if (!(scale >= 0.0f) || !(scale <= 3.0e38f)) return HB_ERR_BAD_ARG;
-  const size_t need = hb_kv8_attention_scratch(r.n_segs, r.Hkv, c->cfg.head_dim, r.max_keys);
+  const size_t need = hb_kv8_attention_scratch(c->cfg, r.n_rows, r.n_segs, r.max_keys, hb_kv8_min_split_keys());
   if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 256))) return HB_ERR_BAD_ARG;
   if (r.n_rows == 0 || r.n_segs == 0 || r.max_q_len == 0) return HB_OK;
   if (!q || !out) return HB_ERR_BAD_ARG;
   if (scale == 0.0f) scale = 1.0f / sqrtf(static_cast<float>(c->cfg.head_dim));
-  return hb_launch_kv8_attention(c, r, q, q_stride, out, out_stride, scale, workspace, static_cast<cudaStream_t>(stream), false);
+  int launches = 0;
+  return hb_launch_kv8_attention(c, r, q, q_stride, out, out_stride, scale, hb_kv8_min_split_keys(), workspace,
+                                 static_cast<cudaStream_t>(stream), false, &launches);
 }
 
 int hb_rope_table(int32_t n_pos, int32_t rot_dim, double theta, const hb_rope_scaling* sc, float* out_cos, float* out_sin) {
@@ -677,7 +687,8 @@ int hb_mixed_step_lora(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, c
   if (!c || !d || !w || !kv || !w->layers || !w->tok_emb || !w->final_norm) return HB_ERR_BAD_ARG;
   if (lora && (lora->rank < 1 || lora->rank > HB_LORA_MAX_RANK || !lora->layers || !(lora->scale == lora->scale)))
     return HB_ERR_BAD_ARG;
-  if (!kv->arena || !kv->has_map) return HB_ERR_BAD_ARG;
+  if (!kv->arena || (!kv->has_map && !kv->e4m3)) return HB_ERR_BAD_ARG;
+  if (kv->e4m3 && d->n_segs > hb_kv8_max_segs()) return HB_ERR_TOO_LARGE;
   if (memcmp(&kv->cfg, &c->cfg, sizeof(hb_model_cfg)) != 0) return HB_ERR_BAD_ARG;
   const int32_t n_slots = pool ? pool->n_slots : 0;
   int rc = validate(c->cfg, c->max_tokens, c->max_segs, c->max_page_ids, kv->n_pages, n_slots,
@@ -873,6 +884,22 @@ int hb_mixed_step_lora(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, c
 
   const int n_qkv = (cfg.n_heads + 2 * cfg.n_kv_heads) * cfg.head_dim;
   const int n_q = cfg.n_heads * cfg.head_dim;
+  // the rows and the layer's pages as the operators over an 8-bit cache see them
+  hb_kv8::Rows r8 = {};
+  hb_append_args ap8 = {};
+  if (kv->e4m3) {
+    hb_rows hr = {};
+    hr.segs = dd.segs; hr.page_ids = dd.pages; hr.row_seg = dd.row_seg;
+    hr.n_segs = R; hr.n_page_ids = d->n_page_ids; hr.n_rows = T;
+    for (int32_t r = 0; r < R; ++r) {
+      hr.max_q_len = std::max(hr.max_q_len, d->segs[r].q_len);
+      hr.max_keys = std::max(hr.max_keys, d->segs[r].pos_start + d->segs[r].q_len);
+    }
+    if ((rc = kv8_rows(c, kv, 0, &hr, &r8)) != HB_OK) return rc;
+    ap8.qkv = c->act; ap8.qkv_stride = n_qkv; ap8.q_out = c->q; ap8.q_stride = n_q;
+    ap8.rope_cos = c->rope_cos; ap8.rope_sin = c->rope_sin; ap8.rope_rows = cfg.max_pos;
+    ap8.rot_dim = cfg.head_dim; ap8.rope_layout = HB_ROPE_PAIRS;
+  }
   // adapters apply to EMBED_CHUNK rows, which are the last rows of the batch (kinds are sorted)
   int32_t first_embed_row = T;
   for (int32_t r = 0; r < R; ++r)
@@ -984,16 +1011,30 @@ int hb_mixed_step_lora(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, c
     ga.P = cfg.page_size; ga.n_pages = kg.n_pages;
     if (use_lora) HB_TRY(HB_CLASS_LORA, lora_down(c->tm_h, lm->a_qkv, r3, cfg.d_model));
     ga.k2_blocks = use_lora ? r3 / 64 : 0;
-    HB_TRY(HB_CLASS_GEMM, hb_gemm_launch(c->tm_h, wm.qkv, v_qkv, HB_EPI_QKV_ROPE, ga, c->num_sms, s,
-                                         use_lora ? &c->tm_lora_u : nullptr, use_lora ? &lm->b_qkv : nullptr, c->pdl));
-    if (ex->profiling) {
-      // timed per class: one launch per item list (the same kernel over one list)
-      if (dd.n_tc_items > 0)
-        HB_TRY(HB_CLASS_ATTENTION_TC, hb_launch_attention(c, kg, kv->map, l, s, HB_ATTN_CHUNK_TILES));
-      if (dd.n_attn_items > 0)
-        HB_TRY(HB_CLASS_ATTENTION, hb_launch_attention(c, kg, kv->map, l, s, HB_ATTN_SMALL_ITEMS));
-    } else if (dd.n_tc_items + dd.n_attn_items > 0) {
-      HB_TRY(HB_CLASS_ATTENTION, hb_launch_attention(c, kg, kv->map, l, s, HB_ATTN_ALL));
+    if (kv->e4m3) {
+      // 8-bit cache: a block's scale needs all its new rows, so the projection leaves plain fp16 rows; one
+      // kernel rotates, quantises and appends them, and the attention reads the 8-bit pages
+      ga.C = c->act;
+      HB_TRY(HB_CLASS_GEMM, hb_gemm_launch(c->tm_h, wm.qkv, v_qkv, HB_EPI_F16, ga, c->num_sms, s,
+                                           use_lora ? &c->tm_lora_u : nullptr, use_lora ? &lm->b_qkv : nullptr, c->pdl));
+      r8.arena = static_cast<uint8_t*>(kv->arena) + l * r8.page_stride * kv->n_pages;
+      HB_TRY(HB_CLASS_NORM_ROPE, hb_launch_kv8_append(c, r8, ap8, s, c->pdl));
+      int n_attn = 0;
+      HB_TRY(HB_CLASS_ATTENTION, hb_launch_kv8_attention(c, r8, c->q, n_q, c->attn_out, n_q, 1.0f / sqrtf(static_cast<float>(cfg.head_dim)),
+                                                         ex->lay.kv8_split_keys, c->act, s, c->pdl, &n_attn));
+      launches += n_attn - 1;
+    } else {
+      HB_TRY(HB_CLASS_GEMM, hb_gemm_launch(c->tm_h, wm.qkv, v_qkv, HB_EPI_QKV_ROPE, ga, c->num_sms, s,
+                                           use_lora ? &c->tm_lora_u : nullptr, use_lora ? &lm->b_qkv : nullptr, c->pdl));
+      if (ex->profiling) {
+        // timed per class: one launch per item list (the same kernel over one list)
+        if (dd.n_tc_items > 0)
+          HB_TRY(HB_CLASS_ATTENTION_TC, hb_launch_attention(c, kg, kv->map, l, s, HB_ATTN_CHUNK_TILES));
+        if (dd.n_attn_items > 0)
+          HB_TRY(HB_CLASS_ATTENTION, hb_launch_attention(c, kg, kv->map, l, s, HB_ATTN_SMALL_ITEMS));
+      } else if (dd.n_tc_items + dd.n_attn_items > 0) {
+        HB_TRY(HB_CLASS_ATTENTION, hb_launch_attention(c, kg, kv->map, l, s, HB_ATTN_ALL));
+      }
     }
     // O projection, added to the residual stream
     ga.C = c->x; ga.N = cfg.d_model; ga.K = n_q; ga.ldc = cfg.d_model;

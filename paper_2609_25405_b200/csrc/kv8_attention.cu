@@ -40,23 +40,30 @@ struct AttnParams {
   __half* out;
   int64_t q_stride, out_stride;
   float scale_log2;
-  int32_t max_splits;   // splits of the longest segment
-  float* part_o;        // [n_segs * Hkv][max_splits][16][DH]: weighted sums relative to their maximum
-  float2* part_ml;      // [n_segs * Hkv][max_splits][16]: maximum (log2), sum
+  int32_t min_split;    // keys of a split, unless the segment is so long that it would have more than MAX_SPLITS
+  int32_t max_splits;   // no segment has more
+  int32_t by_row;       // how the records of a column are numbered: see record()
+  float* part_o;        // [column][max_splits][DH]: weighted sums relative to their maximum
+  float2* part_ml;      // [column][max_splits]: maximum (log2), sum
 };
 
-// Keys per split of a segment with `keys` keys: 512, more once that would be over MAX_SPLITS splits (whole
-// pages for each warp).
-__device__ __forceinline__ int split_keys(int keys) {
+// Keys per split of a segment with `keys` keys: a multiple of the 64 keys that the four warps take in turn.
+__device__ __forceinline__ int split_keys(const AttnParams& p, int keys) {
   const int per = (keys / MAX_SPLITS + 128) / 128 * 128;
-  return per < MIN_SPLIT_KEYS ? MIN_SPLIT_KEYS : per;
+  return per < p.min_split ? p.min_split : per;
 }
-__device__ __forceinline__ int n_splits(int keys) {
-  const int per = split_keys(keys);
+__device__ __forceinline__ int n_splits(const AttnParams& p, int keys) {
+  const int per = split_keys(p, keys);
   return keys <= per ? 1 : (keys - 1) / per + 1;
 }
 // No segment of up to max_keys keys has more splits (the count itself is not monotonic in the keys).
-inline int splits_bound(int max_keys) { return std::max(1, std::min(MAX_SPLITS, max_keys / MIN_SPLIT_KEYS + 1)); }
+inline int splits_bound(int max_keys, int min_split) { return std::max(1, std::min(MAX_SPLITS, max_keys / min_split + 1)); }
+// Columns that can have records: every row's heads, or 16 for each segment and KV head, whichever is less.
+inline size_t record_columns(int n_rows, int n_segs, int n_kv_heads, int group, bool* by_row) {
+  const size_t rows = static_cast<size_t>(n_rows) * n_kv_heads * group, segs = static_cast<size_t>(n_segs) * n_kv_heads * TILE_COLS;
+  *by_row = rows <= segs;
+  return std::min(rows, segs);
+}
 
 struct Seg { int q_start, q_len, pos_start, pt_start; };
 
@@ -68,9 +75,15 @@ __device__ __forceinline__ bool load_seg(const Rows& r, int s, Seg& g) {
 }
 
 // Splits of a segment of the decode body: one to 16 columns (0: no rows, or rows for the chunk body).
-__device__ __forceinline__ int splits_of(const Rows& r, const Seg& g) {
-  const int cols = g.q_len * r.G;
-  return cols < 1 || cols > TILE_COLS ? 0 : n_splits(g.pos_start + g.q_len);
+__device__ __forceinline__ int splits_of(const AttnParams& p, const Seg& g) {
+  const int cols = g.q_len * p.r.G;
+  return cols < 1 || cols > TILE_COLS ? 0 : n_splits(p, g.pos_start + g.q_len);
+}
+// First record of column c of a segment's KV head.
+__device__ __forceinline__ int64_t record(const AttnParams& p, int seg, const Seg& g, int head, int c) {
+  const int64_t column = p.by_row ? static_cast<int64_t>(g.q_start + c / p.r.G) * (p.r.Hkv * p.r.G) + head * p.r.G + c % p.r.G
+                                  : (static_cast<int64_t>(seg) * p.r.Hkv + head) * TILE_COLS + c;
+  return column * p.max_splits;
 }
 
 // Segment that item idx belongs to: prefix[s] <= idx < prefix[s + 1].
@@ -94,11 +107,11 @@ __device__ __forceinline__ void find_item(const AttnParams& p, const int* prefix
   it.seg = find_seg(prefix, p.r.n_segs, idx);
   load_seg(p.r, it.seg, it.g);
   const int keys = it.g.pos_start + it.g.q_len, at = idx - prefix[it.seg];
-  it.ns = splits_of(p.r, it.g);
+  it.ns = splits_of(p, it.g);
   it.head = at % p.r.Hkv;
   it.split = at / p.r.Hkv;
   it.n_cols = it.g.q_len * p.r.G;
-  const int per = it.ns > 1 ? split_keys(keys) : keys;
+  const int per = it.ns > 1 ? split_keys(p, keys) : keys;
   it.key0 = it.split * per;
   it.key1 = min(keys, it.key0 + per);
 }
@@ -367,7 +380,7 @@ __device__ __forceinline__ bool run_item(const AttnParams& p, const Item& it, Ri
     }
   const bool all_ok = __syncthreads_and(ok) != 0;
   if (!all_ok && it.ns > 1 && tid < it.n_cols)   // a negative sum tells the join to leave the row alone
-    p.part_ml[((static_cast<int64_t>(it.seg) * p.r.Hkv + it.head) * p.max_splits + it.split) * TILE_COLS + tid] = make_float2(-INFINITY, -1.0f);
+    p.part_ml[record(p, it.seg, it.g, it.head, tid) + it.split] = make_float2(-INFINITY, -1.0f);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     float f[2];
@@ -408,9 +421,9 @@ __device__ __forceinline__ bool run_item(const AttnParams& p, const Item& it, Ri
           __half* dst = p.out + (it.g.q_start + c / p.r.G) * p.out_stride + (it.head * p.r.G + c % p.r.G) * DH + d;
           *reinterpret_cast<uint32_t*>(dst) = pack_half2_sat(x * inv, y * inv);
         } else {
-          const int64_t rec = (static_cast<int64_t>(it.seg) * p.r.Hkv + it.head) * p.max_splits + it.split;
-          *reinterpret_cast<float2*>(p.part_o + (rec * TILE_COLS + c) * DH + d) = make_float2(x, y);
-          if (d == 0) p.part_ml[rec * TILE_COLS + c] = make_float2(m, l);
+          const int64_t rec = record(p, it.seg, it.g, it.head, c) + it.split;
+          *reinterpret_cast<float2*>(p.part_o + rec * DH + d) = make_float2(x, y);
+          if (d == 0) p.part_ml[rec] = make_float2(m, l);
         }
       }
     }
@@ -437,7 +450,7 @@ kv8_attend_kernel(const AttnParams p) {
   if (tid < DEC_WARPS * STAGES) mbar_init(smem_u32(tail) + 8u * tid, 1);
   if (tid == 0) *abort_flag = 0u;
   mbar_init_fence();
-  const int total = build_prefix<DEC_THREADS>(p.r, prefix, warp_sums, [&](const Seg& g) { return splits_of(p.r, g) * p.r.Hkv; }, true);   // its barriers publish the initialisation
+  const int total = build_prefix<DEC_THREADS>(p.r, prefix, warp_sums, [&](const Seg& g) { return splits_of(p, g) * p.r.Hkv; }, true);   // its barriers publish the initialisation
   for (int idx = blockIdx.x; idx < total; idx += gridDim.x) {
     Item it;
     find_item(p, prefix, idx, it);
@@ -464,22 +477,22 @@ kv8_join_kernel(const AttnParams p, const int cols) {
   const int c = blockIdx.x % cols, head = (blockIdx.x / cols) % p.r.Hkv, seg = blockIdx.x / (cols * p.r.Hkv);
   Seg g;
   if (!load_seg(p.r, seg, g)) return;
-  const int ns = splits_of(p.r, g);
+  const int ns = splits_of(p, g);
   if (ns <= 1 || c >= g.q_len * p.r.G) return;
-  const int64_t rec = (static_cast<int64_t>(seg) * p.r.Hkv + head) * p.max_splits;
+  const int64_t rec = record(p, seg, g, head, c);
   float m = -INFINITY;
   for (int s = 0; s < ns; ++s) {
-    const float2 a = p.part_ml[(rec + s) * TILE_COLS + c];
+    const float2 a = p.part_ml[rec + s];
     if (a.y < 0.0f) return;   // a split that was given up
     m = fmaxf(m, a.x);
   }
   float l = 0.0f, x = 0.0f;
 #pragma unroll 8
   for (int s = 0; s < ns; ++s) {
-    const float2 a = p.part_ml[(rec + s) * TILE_COLS + c];
+    const float2 a = p.part_ml[rec + s];
     const float f = a.x > -INFINITY ? ex2_approx(a.x - m) : 0.0f;
     l = fmaf(a.y, f, l);
-    x = fmaf(p.part_o[((rec + s) * TILE_COLS + c) * DH + threadIdx.x], f, x);
+    x = fmaf(p.part_o[(rec + s) * DH + threadIdx.x], f, x);
   }
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
   p.out[(g.q_start + c / p.r.G) * p.out_stride + (head * p.r.G + c % p.r.G) * DH + threadIdx.x] =
@@ -487,7 +500,7 @@ kv8_join_kernel(const AttnParams p, const int cols) {
 }
 
 template <int DH>
-int launch(const AttnParams& p, int num_sms, cudaStream_t s, bool pdl) {
+int launch(const AttnParams& p, int num_sms, cudaStream_t s, bool pdl, int* launches) {
   static DynSmemState configured;
   const int smem = DecCfg<DH>::FIXED + (p.r.n_segs + 1) * 4;
   if (smem > 227 * 1024) return HB_ERR_TOO_LARGE;
@@ -496,6 +509,7 @@ int launch(const AttnParams& p, int num_sms, cudaStream_t s, bool pdl) {
   // no more blocks than the bounds of the call allow items
   const long long most = static_cast<long long>(p.r.n_segs) * p.r.Hkv * p.max_splits;
   int rc = hb_launch_kernel(kern, static_cast<unsigned>(std::min<long long>(most, 3ll * num_sms)), DEC_THREADS, smem, s, pdl, p);
+  *launches = 1;
   const long long cols_bound = static_cast<long long>(p.r.max_q_len) * p.r.G;
   if (rc == HB_OK && cols_bound > TILE_COLS) {   // segments for the chunk body are possible
     static DynSmemState tc_configured;
@@ -505,26 +519,28 @@ int launch(const AttnParams& p, int num_sms, cudaStream_t s, bool pdl) {
     if (hb_ensure_dyn_smem(reinterpret_cast<const void*>(tc), tc_configured, tc_smem) != HB_OK) return HB_ERR_CUDA;
     const long long tc_most = static_cast<long long>(p.r.n_segs) * p.r.Hkv * ((cols_bound + hb_kv8_tc::ROWS - 1) / hb_kv8_tc::ROWS);
     rc = hb_launch_kernel(tc, static_cast<unsigned>(std::min<long long>(tc_most, num_sms)), hb_kv8_tc::THREADS, tc_smem, s, true, p);
+    ++*launches;
   }
   if (rc != HB_OK || p.max_splits == 1) return rc;
+  ++*launches;
   const int cols = static_cast<int>(std::min<long long>(TILE_COLS, cols_bound));
   return hb_launch_kernel(kv8_join_kernel<DH>, static_cast<unsigned>(p.r.n_segs) * p.r.Hkv * cols, DH, 0, s, true, p, cols);
-}
-
-size_t part_records(int n_segs, int n_kv_heads, int splits) {
-  return splits > 1 ? static_cast<size_t>(n_segs) * n_kv_heads * splits * TILE_COLS : 0;
 }
 
 }  // namespace
 
 int hb_kv8_max_segs() { return MAX_SEGS; }
+int hb_kv8_min_split_keys() { return MIN_SPLIT_KEYS; }
 
-size_t hb_kv8_attention_scratch(int n_segs, int n_kv_heads, int head_dim, int max_keys) {
-  return part_records(n_segs, n_kv_heads, splits_bound(max_keys)) * (static_cast<size_t>(head_dim) * 4 + 8);
+size_t hb_kv8_attention_scratch(const hb_model_cfg& cfg, int n_rows, int n_segs, int max_keys, int min_split) {
+  const int splits = splits_bound(max_keys, min_split);
+  bool by_row;
+  const size_t columns = record_columns(n_rows, n_segs, cfg.n_kv_heads, cfg.n_heads / cfg.n_kv_heads, &by_row);
+  return splits > 1 ? columns * splits * (static_cast<size_t>(cfg.head_dim) * 4 + 8) : 0;
 }
 
 int hb_launch_kv8_attention(hb_ctx* c, const hb_kv8::Rows& r, const void* q, int64_t q_stride, void* out, int64_t out_stride,
-                            float scale, void* workspace, cudaStream_t s, bool pdl) {
+                            float scale, int min_split, void* workspace, cudaStream_t s, bool pdl, int* launches) {
   AttnParams p;
   p.r = r;
   p.q = static_cast<const __half*>(q);
@@ -532,10 +548,14 @@ int hb_launch_kv8_attention(hb_ctx* c, const hb_kv8::Rows& r, const void* q, int
   p.q_stride = q_stride;
   p.out_stride = out_stride;
   p.scale_log2 = scale * 1.4426950408889634f;
-  p.max_splits = splits_bound(r.max_keys);
+  p.min_split = min_split;
+  p.max_splits = splits_bound(r.max_keys, min_split);
+  bool by_row;
+  const size_t columns = record_columns(r.n_rows, r.n_segs, r.Hkv, r.G, &by_row);
+  p.by_row = by_row ? 1 : 0;
   p.part_o = static_cast<float*>(workspace);
-  p.part_ml = reinterpret_cast<float2*>(p.part_o + part_records(r.n_segs, r.Hkv, p.max_splits) * c->cfg.head_dim);
-  if (c->cfg.head_dim == 64) return launch<64>(p, c->num_sms, s, pdl);
-  if (c->cfg.head_dim == 128) return launch<128>(p, c->num_sms, s, pdl);
+  p.part_ml = reinterpret_cast<float2*>(p.part_o + columns * p.max_splits * c->cfg.head_dim);
+  if (c->cfg.head_dim == 64) return launch<64>(p, c->num_sms, s, pdl, launches);
+  if (c->cfg.head_dim == 128) return launch<128>(p, c->num_sms, s, pdl, launches);
   return HB_ERR_UNSUPPORTED;
 }

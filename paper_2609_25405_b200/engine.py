@@ -71,7 +71,10 @@ def build_batch(entries, page_size):
 
 class Engine:
     def __init__(self, shape, weights, n_pages, n_slots, max_tokens, max_segs, max_pos,
-                 kv_fill=None, pool_fill=None, device="cuda", lora=None):
+                 kv_fill=None, pool_fill=None, device="cuda", lora=None, kv_dtype="f16"):
+        """kv_dtype: "f16", or "e4m3" for the 8-bit cache (half the memory per token)."""
+        if kv_dtype not in ("f16", "e4m3"):
+            raise ValueError(f"kv_dtype: 'f16' or 'e4m3', not {kv_dtype!r}")
         self.shape = shape
         self.lora = lora                    # binding.DeviceLora applied to embedding rows, or None
         self.cfg = B.model_cfg(shape, max_pos)
@@ -79,7 +82,7 @@ class Engine:
         self.max_tokens, self.max_segs = max_tokens, max_segs
         max_page_ids = max_segs * ((max_pos + shape.page_size - 1) // shape.page_size)
         self.ctx = B.Context(self.cfg, max_tokens, max_segs, max_page_ids)
-        self.kv = B.KvCache(self.cfg, n_pages, device, fill=kv_fill)
+        self.kv = (B.KvCache8 if kv_dtype == "e4m3" else B.KvCache)(self.cfg, n_pages, device, fill=kv_fill)
         self.pool = B.Pool(self.cfg, n_slots, device, fill=pool_fill)
         self.out_logits = torch.zeros((max_segs, shape.V), dtype=torch.float32, device=device)
         self.out_emb = torch.zeros((max_segs, shape.d), dtype=torch.float32, device=device)

@@ -72,13 +72,14 @@ def test_pages_of_an_8_bit_cache():
 
 def test_workspace_grows_with_the_splits():
     n = C.c_size_t()
-    size = lambda segs, keys: (B.lib.hb_kv8_attention_workspace(C.byref(CFG), C.byref(B.RowsStruct(n_segs=segs, max_keys=keys)),  # noqa: E731
-                                                                C.byref(n)), n.value)
-    assert size(4, 0) == (0, 0) and size(4, 511) == (0, 0)
-    rec = 16 * (TINY.Dh * 4 + 8)
-    assert size(4, 1024) == (0, 4 * TINY.Hkv * 3 * rec)
-    assert size(4, 1 << 20) == (0, 4 * TINY.Hkv * 64 * rec)      # never more than 64 splits
-    assert size(-1, 10)[0] == -1 and size(1, -1)[0] == -1 and size(8193, 10)[0] == -5
+    size = lambda rows, segs, keys: (B.lib.hb_kv8_attention_workspace(C.byref(CFG), C.byref(B.RowsStruct(  # noqa: E731
+        n_rows=rows, n_segs=segs, max_keys=keys)), C.byref(n)), n.value)
+    assert size(4, 4, 0) == (0, 0) and size(4, 4, 511) == (0, 0)
+    rec = TINY.Dh * 4 + 8
+    assert size(4, 4, 1024) == (0, 4 * TINY.Hq * 3 * rec)              # every row's heads ...
+    assert size(1000, 4, 1024) == (0, 4 * TINY.Hkv * 16 * 3 * rec)     # ... or 16 columns per segment and KV head
+    assert size(4, 4, 1 << 20) == (0, 4 * TINY.Hq * 64 * rec)          # never more than 64 splits
+    assert size(-1, 1, 10)[0] == -1 and size(1, -1, 10)[0] == -1 and size(1, 1, -1)[0] == -1 and size(1, 8193, 10)[0] == -5
 
 
 def test_calls_without_a_context_or_cache_are_refused():
