@@ -264,6 +264,30 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// ---- two floats at a time ---------------------------------------------------------------------------
+// Two floats in one 64-bit register pair, and the instructions that work on both.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 // ---- small numeric helpers ----------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   __half2 v = __floats2half2_rn(lo, hi);
@@ -276,6 +300,12 @@ __device__ __forceinline__ float sat_half_range(float v) {
 }
 __device__ __forceinline__ uint32_t pack_half2_sat(float lo, float hi) {
   return pack_half2(sat_half_range(lo), sat_half_range(hi));
+}
+// pack_half2_sat with the clamp behind the conversion, on both halves at once (an overflow is infinite there).
+__device__ __forceinline__ uint32_t pack_half2_sat2(float lo, float hi) {
+  uint32_t v = pack_half2(lo, hi);
+  asm("{\n\tmax.NaN.f16x2 %0, %0, %1;\n\tmin.NaN.f16x2 %0, %0, %2;\n\t}" : "+r"(v) : "r"(0xfbfffbffu), "r"(0x7bff7bffu));
+  return v;
 }
 // True when v does not fit a finite half: NaN, infinite, or beyond +-65504.
 __device__ __forceinline__ bool outside_half_range(float v) { return !(fabsf(v) <= 65504.0f); }
