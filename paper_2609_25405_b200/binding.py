@@ -462,7 +462,7 @@ class KvCache8(KvCache):
                 self.arena = torch.empty(nbytes, dtype=torch.uint8, device=device)
             if fill is not None:
                 self.arena.fill_(fill)
-        self.device = self.arena.device if self.arena is not None else None
+        self.index = self.arena.get_device() if self.arena is not None else -1
         ptr = C.c_void_p(self.arena.data_ptr()) if self.arena is not None else None
         check(lib.hb_kv8_create(C.byref(cfg), ptr, nbytes, n_pages, C.byref(self.handle)), "hb_kv8_create")
 
@@ -508,7 +508,7 @@ class SegRows:
         if segs.dim() != 2 or segs.shape[1] != 12 or page_ids.dim() != 1 or row_seg.dim() != 1:
             raise ValueError("segs [R, 12], page_ids [n], row_seg [T]")
         self.segs, self.page_ids, self.row_seg = segs, page_ids, row_seg
-        self.device = segs.device
+        self.index = segs.get_device()
         self._need = {}            # workspace bytes by (n_kv_heads, head_dim)
         self.struct = RowsStruct(segs.data_ptr(), page_ids.data_ptr(), row_seg.data_ptr(), segs.shape[0],
                                  page_ids.shape[0], row_seg.shape[0], int(max_q_len), int(max_keys))
@@ -557,13 +557,14 @@ def rope_table(n_pos, rot_dim, theta, scaling=None):
     return cos, sin
 
 
-def _rows_f16(t, rows, cols, device, name):
+def _rows_f16(t, rows, cols, device_index, name):
     """A [>= rows, cols] fp16 matrix with unit column stride: (pointer, row stride)."""
-    if t.dtype is not torch.float16 or t.device != device or t.dim() != 2 or t.size(0) < rows or t.size(1) != cols or \
-            (t.stride(1) != 1 and rows > 0):
-        raise ValueError(f"{name}: an fp16 tensor [{rows}, {cols}] with unit column stride on {device}")
-    stride = t.stride(0)
-    return t.data_ptr(), (stride if rows > 1 or stride >= cols else cols)
+    if t.dtype is torch.float16 and t.get_device() == device_index and t.dim() == 2:
+        have, c = t.shape
+        stride, unit = t.stride()
+        if c == cols and have >= rows and (unit == 1 or rows == 0):
+            return t.data_ptr(), (stride if rows > 1 or stride >= cols else cols)
+    raise ValueError(f"{name}: an fp16 tensor [{rows}, {cols}] with unit column stride on cuda:{device_index}")
 
 
 class Pool:
@@ -653,7 +654,8 @@ class Context:
             raise RuntimeError("libhb needs a CUDA device (B200); there is no CPU path")
         self.cfg = cfg
         self.handle = C.c_void_p()
-        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.index = torch.cuda.current_device()
+        self.device = torch.device("cuda", self.index)
         check(lib.hb_create(C.byref(cfg), max_tokens, max_segs, max_page_ids, None, 0, C.byref(self.handle)),
               "hb_create")
 
@@ -675,11 +677,11 @@ class Context:
         """hb_logprobs: logits fp32 or fp16 [n, vocab] (rows may be strided), tokens int32 [n] (negative = none),
         out_logprob fp32 [n] (tokens and out_logprob both or neither None), out_entropy fp32 [n], and the
         k = out_top_ids.shape[1] best alternatives: out_top_ids int32 [n, k], out_top_logprobs fp32 [n, k]."""
-        dev, dt = self.device, logits.dtype
-        if logits.dim() != 2 or (dt is not torch.float32 and dt is not torch.float16) or logits.device != dev or \
+        dev, dt = self.index, logits.dtype
+        if logits.dim() != 2 or (dt is not torch.float32 and dt is not torch.float16) or logits.get_device() != dev or \
                 (logits.stride(1) != 1 and logits.numel()):
-            raise ValueError(f"logits: fp32 or fp16 [n, vocab] with unit column stride on {dev}")
-        n, vocab = logits.size(0), logits.size(1)
+            raise ValueError(f"logits: fp32 or fp16 [n, vocab] with unit column stride on {self.device}")
+        n, vocab = logits.shape
         k = 0 if out_top_ids is None else out_top_ids.size(-1)
         tp = self._vector(tokens, torch.int32, n, 1, "tokens")
         lp = self._vector(out_logprob, torch.float32, n, 1, "out_logprob")
@@ -690,7 +692,7 @@ class Context:
         if n <= 1 and stride < vocab:
             stride = vocab
         rc = lib.hb_logprobs(self.handle, logits.data_ptr(), DTYPE_F32 if dt is torch.float32 else DTYPE_F16, n, vocab, stride, tp,
-                             k, lp, ep, ip, vp, _stream_of(stream, dev.index))
+                             k, lp, ep, ip, vp, _stream_of(stream, dev))
         if rc != HB_OK:
             raise HbError(rc, "hb_logprobs")
 
@@ -698,7 +700,7 @@ class Context:
         """Pointer of a contiguous [n] (k = 1) or [n, k] tensor, or None."""
         if t is None:
             return None
-        if t.dtype is not dtype or t.device != self.device or t.dim() > 2 or t.size(0) != n or t.numel() != n * k or not t.is_contiguous():
+        if t.dtype is not dtype or t.get_device() != self.index or t.dim() > 2 or t.size(0) != n or t.numel() != n * k or not t.is_contiguous():
             raise ValueError(f"{name}: a contiguous {dtype} tensor of {n} x {k} on {self.device}")
         return t.data_ptr()
 
@@ -721,9 +723,9 @@ class Context:
     def _same_device(self, rows, kv):
         if not isinstance(kv, KvCache8):
             raise TypeError("an 8-bit cache (KvCache8)")
-        if rows.device != self.device or kv.device != self.device:
+        if rows.index != self.index or kv.index != self.index:
             raise ValueError(f"rows and cache on the context's device, {self.device}")
-        return self.device
+        return self.index
 
     def kv8_append(self, kv, layer, rows, qkv, q_out, rope=None, q_norm=None, k_norm=None, norm_eps=1e-6, stream=None):
         """hb_kv8_append: head norms (bf16 gains [Dh] or None), rotation (Rope or None), K / V of every row of
@@ -735,18 +737,18 @@ class Context:
         a.qkv, a.qkv_stride = _rows_f16(qkv, T, (c.n_heads + 2 * c.n_kv_heads) * c.head_dim, dev, "qkv")
         a.q_out, a.q_stride = _rows_f16(q_out, T, c.n_heads * c.head_dim, dev, "q_out")
         for gain, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-            if gain is not None and (gain.dtype != torch.bfloat16 or gain.device != dev or gain.shape != (c.head_dim,) or
+            if gain is not None and (gain.dtype != torch.bfloat16 or gain.get_device() != dev or gain.shape != (c.head_dim,) or
                                      not gain.is_contiguous()):
-                raise ValueError(f"{name}: a bf16 tensor [{c.head_dim}] on {dev}")
+                raise ValueError(f"{name}: a bf16 tensor [{c.head_dim}] on cuda:{dev}")
         a.q_gain = q_norm.data_ptr() if q_norm is not None else None
         a.k_gain = k_norm.data_ptr() if k_norm is not None else None
         a.norm_eps = norm_eps
         if rope is not None:
-            if rope.cos.device != dev:
-                raise ValueError(f"rope: tables on {dev}")
+            if rope.cos.get_device() != dev:
+                raise ValueError(f"rope: tables on cuda:{dev}")
             a.rope_cos, a.rope_sin = rope.cos.data_ptr(), rope.sin.data_ptr()
             a.rope_rows, a.rot_dim, a.rope_layout = rope.cos.shape[0], 2 * rope.cos.shape[1], rope.layout
-        rc = lib.hb_kv8_append(self.handle, kv.handle, layer, C.byref(rows.struct), C.byref(a), _stream_of(stream, dev.index))
+        rc = lib.hb_kv8_append(self.handle, kv.handle, layer, C.byref(rows.struct), C.byref(a), _stream_of(stream, dev))
         if rc != HB_OK:
             raise HbError(rc, "hb_kv8_append")
 
@@ -761,13 +763,13 @@ class Context:
         need, ws, wp = rows.workspace_bytes(c), None, None
         if need:   # allocated on the stream of the call, whose order then protects its reuse
             if stream is None:
-                ws = torch.empty(need, dtype=torch.uint8, device=dev)
+                ws = torch.empty(need, dtype=torch.uint8, device=self.device)
             else:
                 with torch.cuda.stream(stream):
-                    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+                    ws = torch.empty(need, dtype=torch.uint8, device=self.device)
             wp = ws.data_ptr()
         rc = lib.hb_kv8_attention(self.handle, kv.handle, layer, C.byref(rows.struct), qp, qs, op, os_, scale, wp, need,
-                                  _stream_of(stream, dev.index))
+                                  _stream_of(stream, dev))
         if rc != HB_OK:
             raise HbError(rc, "hb_kv8_attention")
 

@@ -28,9 +28,9 @@ using namespace hb_kv8;
 
 constexpr int DEC_WARPS = 4;
 constexpr int DEC_THREADS = DEC_WARPS * 32;
-constexpr int STAGES = 3;
+constexpr int STAGES = 2;   // page blocks of a warp in flight or in use: 16 warps of an SM keep up to 128 KiB
 constexpr int TILE_COLS = 16;
-constexpr int MIN_SPLIT_KEYS = 512, MAX_SPLITS = 64;
+constexpr int MIN_SPLIT_KEYS = 512, MAX_SPLITS = 128;
 constexpr int MAX_SEGS = 8192;
 constexpr uint64_t WAIT_NS = 1000000000ull;
 
@@ -47,16 +47,17 @@ struct AttnParams {
   float2* part_ml;      // [column][max_splits]: maximum (log2), sum
 };
 
-// Keys per split of a segment with `keys` keys: a multiple of the 64 keys that the four warps take in turn.
+// Keys per split of a segment with `keys` keys: as few splits of at most min_split keys as there can be (no
+// more than MAX_SPLITS), of equal size, a multiple of the 64 keys that the four warps take in turn.
 __device__ __forceinline__ int split_keys(const AttnParams& p, int keys) {
-  const int per = (keys / MAX_SPLITS + 128) / 128 * 128;
-  return per < p.min_split ? p.min_split : per;
+  const int n = min(MAX_SPLITS, max(1, (keys + p.min_split - 1) / p.min_split));
+  return ((keys + n - 1) / n + 63) / 64 * 64;
 }
 __device__ __forceinline__ int n_splits(const AttnParams& p, int keys) {
   const int per = split_keys(p, keys);
   return keys <= per ? 1 : (keys - 1) / per + 1;
 }
-// No segment of up to max_keys keys has more splits (the count itself is not monotonic in the keys).
+// No segment of up to max_keys keys has more splits.
 inline int splits_bound(int max_keys, int min_split) { return std::max(1, std::min(MAX_SPLITS, max_keys / min_split + 1)); }
 // Columns that can have records: every row's heads, or 16 for each segment and KV head, whichever is less.
 inline size_t record_columns(int n_rows, int n_segs, int n_kv_heads, int group, bool* by_row) {
@@ -101,6 +102,7 @@ struct Item {
   int seg, head, split, ns;
   int n_cols;
   int key0, key1;     // keys [key0, key1) of this split
+  int all_see;        // last key of the split that every column sees
 };
 
 __device__ __forceinline__ void find_item(const AttnParams& p, const int* prefix, int idx, Item& it) {
@@ -114,6 +116,7 @@ __device__ __forceinline__ void find_item(const AttnParams& p, const int* prefix
   const int per = it.ns > 1 ? split_keys(p, keys) : keys;
   it.key0 = it.split * per;
   it.key1 = min(keys, it.key0 + per);
+  it.all_see = min(it.key1 - 1, it.g.pos_start);
 }
 
 // prefix[s] = items before segment s (items(segment) each); returns the total.  All threads of the block; ends
@@ -161,8 +164,8 @@ template <int DH>
 struct DecCfg {
   static constexpr int BLK = Block<DH>::BYTES;
   static constexpr int RING = DEC_WARPS * STAGES * BLK;
-  static constexpr int ROW = DH + 4;   // floats per column of the merge buffer (the odd quarter keeps the stores conflict-free)
-  static constexpr int MERGE = DEC_WARPS * 8 * ROW * 4;          // one 8-column tile at a time
+  static constexpr int ROW = 64 + 4;   // floats per column of the merge buffer (the odd quarter keeps the stores conflict-free)
+  static constexpr int MERGE = DEC_WARPS * 8 * ROW * 4;          // 64 dimensions of one 8-column tile at a time
   static constexpr int ML = DEC_WARPS * TILE_COLS * 8;
   static constexpr int BARS = DEC_WARPS * STAGES * 8;
   static constexpr int FIXED = RING + MERGE + ML + BARS + 64;
@@ -224,9 +227,10 @@ __device__ __forceinline__ void page_step(const AttnParams& p, const Item& it, u
   ks *= p.scale_log2;
   const int ev = exponent_of(vs);
   const float fev = static_cast<float>(ev), back = pow2f(max(-126, min(126, -ev)));
-  float s[NT][4];
+  // (two chains of accumulation: a matrix instruction waits for the one before it on the same sum)
+  float s[NT][4], s1[NT][4];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
+  for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = s1[nt][0] = s1[nt][1] = s1[nt][2] = s1[nt][3] = 0.0f;
 #pragma unroll
   for (int hf = 0; hf < DH / 64; ++hf) {
     const uint4 ka = lds128(blk + hf * 1024 + g * 64 + t * 16), kb = lds128(blk + hf * 1024 + (g + 8) * 64 + t * 16);
@@ -237,19 +241,28 @@ __device__ __forceinline__ void page_step(const AttnParams& p, const Item& it, u
       e4m3x4_to_half2x2(wa[w], a[0], a[2]);
       e4m3x4_to_half2x2(wb[w], a[1], a[3]);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], a, st.q[nt][hf * 4 + w][0], st.q[nt][hf * 4 + w][1]);
+      for (int nt = 0; nt < NT; ++nt) mma_f16((w & 1) ? s1[nt] : s[nt], a, st.q[nt][hf * 4 + w][0], st.q[nt][hf * 4 + w][1]);
     }
   }
-  // scores in the log2 domain, plus V's exponent; invisible keys -inf
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[nt][e] += s1[nt][e];
+  // scores in the log2 domain, plus V's exponent; invisible keys (only in pages that reach behind the last key
+  // that every column sees) -inf
+  const bool masked = key + PAGE - 1 > it.all_see;
   bool grow = false;
   float mx[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const bool v0 = key + g <= st.lim[nt][e], v1 = key + g + 8 <= st.lim[nt][e];
-      s[nt][e] = v0 ? fmaf(s[nt][e], ks, fev) : -INFINITY;
-      s[nt][2 + e] = v1 ? fmaf(s[nt][2 + e], ks, fev) : -INFINITY;
+      s[nt][e] = fmaf(s[nt][e], ks, fev);
+      s[nt][2 + e] = fmaf(s[nt][2 + e], ks, fev);
+      if (masked) {
+        if (key + g > st.lim[nt][e]) s[nt][e] = -INFINITY;
+        if (key + g + 8 > st.lim[nt][e]) s[nt][2 + e] = -INFINITY;
+      }
       float m = fmaxf(s[nt][e], s[nt][2 + e]);
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
@@ -297,14 +310,19 @@ __device__ __forceinline__ void page_step(const AttnParams& p, const Item& it, u
   // tokens past the request's last key hold whatever was there: their codes become zero (0 * NaN is NaN)
   uint32_t keep = 0xffffffffu;
   const int left = it.g.pos_start + it.g.q_len - key;
-  if (left < PAGE) {
+  const bool short_page = left < PAGE;
+  if (short_page) {
     keep = (2 * t < left ? 0xffu : 0u) | (2 * t + 1 < left ? 0xff00u : 0u) | (2 * t + 8 < left ? 0xff0000u : 0u) |
            (2 * t + 9 < left ? 0xff000000u : 0u);
   }
 #pragma unroll
   for (int c = 0; c < DH / 32; ++c) {
     const uint4 v = lds128(blk + Block<DH>::V_OFF + c * 512 + lane * 16);
-    const uint32_t wv[4] = {v.x & keep, v.y & keep, v.z & keep, v.w & keep};
+    uint32_t wv[4] = {v.x, v.y, v.z, v.w};
+    if (short_page) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) wv[w] &= keep;
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       uint32_t a[4];
@@ -335,36 +353,54 @@ __device__ __forceinline__ void request(const AttnParams& p, Ring& ring, int pag
   ++ring.n;
 }
 
-template <int DH, int NT>
-__device__ __forceinline__ bool run_item(const AttnParams& p, const Item& it, Ring& ring, uint8_t* smem, volatile uint32_t* abort_flag) {
+// A warp's pages of an item: every fourth.
+__device__ __forceinline__ int warp_pages(const Item& it) {
+  const int warp = threadIdx.x >> 5, n = (it.key1 + PAGE - 1) / PAGE - it.key0 / PAGE;
+  return n > warp ? (n - warp + DEC_WARPS - 1) / DEC_WARPS : 0;
+}
+// Page ids of the warp's pages [batch, batch + 32) of an item, one per lane (-2: none).
+__device__ __forceinline__ int load_ids(const AttnParams& p, const Item& it, int batch) {
+  const int i = batch + (threadIdx.x & 31);
+  return i < warp_pages(it) ? __ldg(p.r.page_ids + it.g.pt_start + it.key0 / PAGE + (threadIdx.x >> 5) + i * DEC_WARPS) : -2;
+}
+// Checks a batch of ids and asks for its first pages.  False (and a report) if one is no page: nothing is asked for.
+template <int DH>
+__device__ __forceinline__ bool start_batch(const AttnParams& p, const Item& it, int id, int n, Ring& ring) {
+  if (__any_sync(0xffffffffu, id != -2 && (id < 0 || id >= p.r.n_pages))) {
+    if ((threadIdx.x & 31) == 0) atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
+    return false;
+  }
+  for (int i = 0; i < min(n, STAGES); ++i) request<DH>(p, ring, __shfl_sync(0xffffffffu, id, i), it.head);
+  return true;
+}
+
+// One item; its first batch of pages (`id`) has been started (`ok`).  `before_join` runs when the last page has
+// been computed: it starts the next item's pages, which then arrive while the warps are joined.
+template <int DH, int NT, class F>
+__device__ __forceinline__ bool run_item(const AttnParams& p, const Item& it, int id, bool ok, Ring& ring, uint8_t* smem, volatile uint32_t* abort_flag,
+                                         F&& before_join) {
   using C = DecCfg<DH>;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   State<DH, NT> st;
   begin<DH, NT>(p, it, st);
-  const int pg0 = it.key0 / PAGE, pg1 = (it.key1 + PAGE - 1) / PAGE;
-  const int mine = pg1 - pg0 > warp ? (pg1 - pg0 - warp + DEC_WARPS - 1) / DEC_WARPS : 0;
-  bool ok = true;
+  const int mine = warp_pages(it), pg0 = it.key0 / PAGE + warp;
   for (int batch = 0; batch < mine && ok; batch += 32) {
-    // page ids of the warp's next 32 pages, one per lane
     const int nb = min(32, mine - batch);
-    int id = -1;
-    if (lane < nb) id = __ldg(p.r.page_ids + it.g.pt_start + pg0 + warp + (batch + lane) * DEC_WARPS);
-    if (__any_sync(0xffffffffu, lane < nb && (id < 0 || id >= p.r.n_pages))) {
-      if (lane == 0) atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
-      ok = false;
-      break;
+    if (batch > 0) {
+      id = load_ids(p, it, batch);
+      ok = start_batch<DH>(p, it, id, nb, ring);
+      if (!ok) break;
     }
-    int asked = 0;
-    for (; asked < min(nb, STAGES); ++asked) request<DH>(p, ring, __shfl_sync(0xffffffffu, id, asked), it.head);
     for (int i = 0; i < nb; ++i) {
       const uint32_t sg = ring.c % STAGES;
       if (!__all_sync(0xffffffffu, mbar_wait(ring.bar + 8u * sg, (ring.c / STAGES) & 1u, abort_flag, WAIT_NS))) { ok = false; break; }
-      page_step<DH, NT>(p, it, ring.buf + sg * Block<DH>::BYTES, (pg0 + warp + (batch + i) * DEC_WARPS) * PAGE, st);
+      page_step<DH, NT>(p, it, ring.buf + sg * Block<DH>::BYTES, (pg0 + (batch + i) * DEC_WARPS) * PAGE, st);
       ++ring.c;
       __syncwarp();   // every lane has read the stage
-      if (asked < nb) { request<DH>(p, ring, __shfl_sync(0xffffffffu, id, asked), it.head); ++asked; }
+      if (i + STAGES < nb) request<DH>(p, ring, __shfl_sync(0xffffffffu, id, i + STAGES), it.head);
     }
   }
+  if (!*abort_flag) before_join();
   // ---- join the four warps: common maximum, then the weighted sums through shared memory ----
   float* merge = reinterpret_cast<float*>(smem + C::RING);
   float2* ml = reinterpret_cast<float2*>(smem + C::RING + C::MERGE);
@@ -391,51 +427,59 @@ __device__ __forceinline__ bool run_item(const AttnParams& p, const Item& it, Ri
       for (int w = 0; w < DEC_WARPS; ++w) m = fmaxf(m, ml[w * TILE_COLS + nt * 8 + 2 * t + e].x);
       f[e] = st.m[nt][e] == -INFINITY ? 0.0f : ex2_approx(st.m[nt][e] - m);
     }
-    float* mine_at = merge + (warp * 8 + 2 * t) * C::ROW + g;
 #pragma unroll
-    for (int mt = 0; mt < DH / 16; ++mt) {
-      mine_at[mt * 16] = st.o[nt][mt][0] * f[0];
-      mine_at[C::ROW + mt * 16] = st.o[nt][mt][1] * f[1];
-      mine_at[mt * 16 + 8] = st.o[nt][mt][2] * f[0];
-      mine_at[C::ROW + mt * 16 + 8] = st.o[nt][mt][3] * f[1];
-    }
-    __syncthreads();
-    if (all_ok) {
-      // two neighbouring dimensions per thread
-      for (int u = tid; u < 8 * (DH / 2); u += DEC_THREADS) {
-        const int cc = u / (DH / 2), d = (u % (DH / 2)) * 2, c = nt * 8 + cc;
-        if (c >= it.n_cols) continue;
-        float m = -INFINITY, l = 0.0f, x = 0.0f, y = 0.0f;
+    for (int hf = 0; hf < DH / 64; ++hf) {
+      float* mine_at = merge + (warp * 8 + 2 * t) * C::ROW + g;
 #pragma unroll
-        for (int w = 0; w < DEC_WARPS; ++w) m = fmaxf(m, ml[w * TILE_COLS + c].x);
+      for (int m4 = 0; m4 < 4; ++m4) {
+        const int mt = hf * 4 + m4;
+        mine_at[m4 * 16] = st.o[nt][mt][0] * f[0];
+        mine_at[C::ROW + m4 * 16] = st.o[nt][mt][1] * f[1];
+        mine_at[m4 * 16 + 8] = st.o[nt][mt][2] * f[0];
+        mine_at[C::ROW + m4 * 16 + 8] = st.o[nt][mt][3] * f[1];
+      }
+      __syncthreads();
+      if (all_ok) {
+        // two neighbouring dimensions per thread
 #pragma unroll
-        for (int w = 0; w < DEC_WARPS; ++w) {
-          const float2 a = ml[w * TILE_COLS + c];
-          if (a.x > -INFINITY) l = fmaf(a.y, ex2_approx(a.x - m), l);
-          const float2 b = *reinterpret_cast<const float2*>(merge + (w * 8 + cc) * C::ROW + d);
-          x += b.x;
-          y += b.y;
-        }
-        if (it.ns == 1) {
-          const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-          __half* dst = p.out + (it.g.q_start + c / p.r.G) * p.out_stride + (it.head * p.r.G + c % p.r.G) * DH + d;
-          *reinterpret_cast<uint32_t*>(dst) = pack_half2_sat(x * inv, y * inv);
-        } else {
-          const int64_t rec = record(p, it.seg, it.g, it.head, c) + it.split;
-          *reinterpret_cast<float2*>(p.part_o + rec * DH + d) = make_float2(x, y);
-          if (d == 0) p.part_ml[rec] = make_float2(m, l);
+        for (int u = tid; u < 8 * 32; u += DEC_THREADS) {
+          const int cc = u / 32, d = (u % 32) * 2, c = nt * 8 + cc;
+          if (c >= it.n_cols) continue;
+          float m = -INFINITY, l = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+          for (int w = 0; w < DEC_WARPS; ++w) m = fmaxf(m, ml[w * TILE_COLS + c].x);
+#pragma unroll
+          for (int w = 0; w < DEC_WARPS; ++w) {
+            const float2 a = ml[w * TILE_COLS + c];
+            if (a.x > -INFINITY) l = fmaf(a.y, ex2_approx(a.x - m), l);
+            const float2 b = *reinterpret_cast<const float2*>(merge + (w * 8 + cc) * C::ROW + d);
+            x += b.x;
+            y += b.y;
+          }
+          if (it.ns == 1) {
+            const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+            __half* dst = p.out + (it.g.q_start + c / p.r.G) * p.out_stride + (it.head * p.r.G + c % p.r.G) * DH + hf * 64 + d;
+            *reinterpret_cast<uint32_t*>(dst) = pack_half2_sat(x * inv, y * inv);
+          } else {
+            const int64_t rec = record(p, it.seg, it.g, it.head, c) + it.split;
+            *reinterpret_cast<float2*>(p.part_o + rec * DH + hf * 64 + d) = make_float2(x, y);
+            if (hf == 0 && d == 0) p.part_ml[rec] = make_float2(m, l);
+          }
         }
       }
+      __syncthreads();
     }
-    __syncthreads();
   }
   return all_ok;
 }
 
-template <int DH>
-__global__ void __launch_bounds__(DEC_THREADS, 3)
+// MAX_NT: 8-column tiles that a segment of the launch may have.  With one the blocks need fewer registers, and
+// one more fits an SM; the arithmetic of a segment is the same in both.
+template <int DH, int MAX_NT>
+__global__ void __launch_bounds__(DEC_THREADS, MAX_NT == 1 ? 4 : 3)
 kv8_attend_kernel(const AttnParams p) {
   grid_dep_wait();
+  grid_dep_launch();   // (what follows waits for this kernel's end before it reads or writes)
   using C = DecCfg<DH>;
   extern __shared__ __align__(128) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5;
@@ -451,10 +495,33 @@ kv8_attend_kernel(const AttnParams p) {
   if (tid == 0) *abort_flag = 0u;
   mbar_init_fence();
   const int total = build_prefix<DEC_THREADS>(p.r, prefix, warp_sums, [&](const Seg& g) { return splits_of(p, g) * p.r.Hkv; }, true);   // its barriers publish the initialisation
+  Item it;
+  int id = -2;
+  bool ok = true;
+  if (static_cast<int>(blockIdx.x) < total) {
+    find_item(p, prefix, blockIdx.x, it);
+    id = load_ids(p, it, 0);
+    ok = start_batch<DH>(p, it, id, warp_pages(it), ring);
+  }
   for (int idx = blockIdx.x; idx < total; idx += gridDim.x) {
-    Item it;
-    find_item(p, prefix, idx, it);
-    const bool ok = it.n_cols <= 8 ? run_item<DH, 1>(p, it, ring, smem, abort_flag) : run_item<DH, 2>(p, it, ring, smem, abort_flag);
+    // the next item and its page ids are looked up before this one's pages are computed
+    const int next = idx + gridDim.x;
+    Item nit = it;
+    int nid = -2;
+    bool nok = true;
+    if (next < total) {
+      find_item(p, prefix, next, nit);
+      nid = load_ids(p, nit, 0);
+    }
+    auto start_next = [&]() {
+      if (next < total) nok = start_batch<DH>(p, nit, nid, warp_pages(nit), ring);
+    };
+    // (a bad page id costs its item only)
+    if (MAX_NT == 1 || it.n_cols <= 8) run_item<DH, 1>(p, it, id, ok, ring, smem, abort_flag, start_next);
+    else run_item<DH, MAX_NT>(p, it, id, ok, ring, smem, abort_flag, start_next);
+    it = nit;
+    id = nid;
+    ok = nok;
     if (*abort_flag) {
       // a wait ran out: report, let requested copies land, leave
       if (tid == 0) {
@@ -464,53 +531,76 @@ kv8_attend_kernel(const AttnParams p) {
       __syncthreads();
       break;
     }
-    (void)ok;   // a bad page id costs this item only (nothing of it is in flight: ids are checked before the copies)
   }
-  grid_dep_launch();
 }
 
-// Joins the splits of one (segment, KV head, column): thread = dimension, split order fixed.
+// Joins the splits of one segment and KV head, a column per warp, in split order.
+constexpr int JOIN_WARPS = 4;
 template <int DH>
-__global__ void __launch_bounds__(DH)
-kv8_join_kernel(const AttnParams p, const int cols) {
-  grid_dep_wait();
-  const int c = blockIdx.x % cols, head = (blockIdx.x / cols) % p.r.Hkv, seg = blockIdx.x / (cols * p.r.Hkv);
+__global__ void __launch_bounds__(JOIN_WARPS * 32)
+kv8_join_kernel(const AttnParams p) {
+  grid_dep_launch();
+  const int seg = blockIdx.x / p.r.Hkv, head = blockIdx.x % p.r.Hkv, lane = threadIdx.x & 31;
   Seg g;
-  if (!load_seg(p.r, seg, g)) return;
-  const int ns = splits_of(p, g);
-  if (ns <= 1 || c >= g.q_len * p.r.G) return;
-  const int64_t rec = record(p, seg, g, head, c);
-  float m = -INFINITY;
-  for (int s = 0; s < ns; ++s) {
-    const float2 a = p.part_ml[rec + s];
-    if (a.y < 0.0f) return;   // a split that was given up
-    m = fmaxf(m, a.x);
+  const int ns = load_seg(p.r, seg, g) ? splits_of(p, g) : 0;   // (the rows are inputs: they are there before the records)
+  grid_dep_wait();   // every block, so that this grid does not end before the ones in front of it
+  if (ns <= 1) return;
+  constexpr int V = DH / 32;   // dimensions per lane
+  for (int c = threadIdx.x >> 5; c < g.q_len * p.r.G; c += JOIN_WARPS) {
+    const int64_t rec = record(p, seg, g, head, c);
+    // the splits' maxima and sums, up to four per lane
+    constexpr int N = MAX_SPLITS / 32;
+    float2 ml[N];
+    float m = -INFINITY;
+    bool gone = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      ml[i] = lane + 32 * i < ns ? p.part_ml[rec + lane + 32 * i] : make_float2(-INFINITY, 0.0f);
+      gone |= ml[i].y < 0.0f;
+      m = fmaxf(m, ml[i].x);
+    }
+    if (__any_sync(0xffffffffu, gone)) continue;   // a split that was given up
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float l = 0.0f, x[V] = {};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float fm = ml[i].x > -INFINITY ? ex2_approx(ml[i].x - m) : 0.0f;
+      const int here = min(32, ns - 32 * i);
+#pragma unroll 4
+      for (int s = 0; s < here; ++s) {
+        const float f = __shfl_sync(0xffffffffu, fm, s);
+        l = fmaf(__shfl_sync(0xffffffffu, ml[i].y, s), f, l);
+        const float* src = p.part_o + (rec + 32 * i + s) * DH + lane * V;
+        if (V == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(src);
+          x[0] = fmaf(v.x, f, x[0]); x[1] = fmaf(v.y, f, x[1]); x[2 % V] = fmaf(v.z, f, x[2 % V]); x[3 % V] = fmaf(v.w, f, x[3 % V]);
+        } else {
+          const float2 v = *reinterpret_cast<const float2*>(src);
+          x[0] = fmaf(v.x, f, x[0]); x[1] = fmaf(v.y, f, x[1]);
+        }
+      }
+    }
+    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    __half* dst = p.out + (g.q_start + c / p.r.G) * p.out_stride + (head * p.r.G + c % p.r.G) * DH + lane * V;
+#pragma unroll
+    for (int i = 0; i < V; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack_half2_sat(x[i] * inv, x[i + 1] * inv);
   }
-  float l = 0.0f, x = 0.0f;
-#pragma unroll 8
-  for (int s = 0; s < ns; ++s) {
-    const float2 a = p.part_ml[rec + s];
-    const float f = a.x > -INFINITY ? ex2_approx(a.x - m) : 0.0f;
-    l = fmaf(a.y, f, l);
-    x = fmaf(p.part_o[(rec + s) * DH + threadIdx.x], f, x);
-  }
-  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-  p.out[(g.q_start + c / p.r.G) * p.out_stride + (head * p.r.G + c % p.r.G) * DH + threadIdx.x] =
-      __float2half_rn(sat_half_range(x * inv));
 }
 
 template <int DH>
 int launch(const AttnParams& p, int num_sms, cudaStream_t s, bool pdl, int* launches) {
-  static DynSmemState configured;
+  static DynSmemState configured[2];
   const int smem = DecCfg<DH>::FIXED + (p.r.n_segs + 1) * 4;
   if (smem > 227 * 1024) return HB_ERR_TOO_LARGE;
-  auto kern = kv8_attend_kernel<DH>;
-  if (hb_ensure_dyn_smem(reinterpret_cast<const void*>(kern), configured, smem) != HB_OK) return HB_ERR_CUDA;
+  const long long cols_bound = static_cast<long long>(p.r.max_q_len) * p.r.G;
+  const bool narrow = cols_bound <= 8;
+  auto kern = narrow ? kv8_attend_kernel<DH, 1> : kv8_attend_kernel<DH, 2>;
+  if (hb_ensure_dyn_smem(reinterpret_cast<const void*>(kern), configured[narrow], smem) != HB_OK) return HB_ERR_CUDA;
   // no more blocks than the bounds of the call allow items
   const long long most = static_cast<long long>(p.r.n_segs) * p.r.Hkv * p.max_splits;
-  int rc = hb_launch_kernel(kern, static_cast<unsigned>(std::min<long long>(most, 3ll * num_sms)), DEC_THREADS, smem, s, pdl, p);
+  int rc = hb_launch_kernel(kern, static_cast<unsigned>(std::min<long long>(most, (narrow ? 4ll : 3ll) * num_sms)), DEC_THREADS, smem, s, pdl, p);
   *launches = 1;
-  const long long cols_bound = static_cast<long long>(p.r.max_q_len) * p.r.G;
   if (rc == HB_OK && cols_bound > TILE_COLS) {   // segments for the chunk body are possible
     static DynSmemState tc_configured;
     const int tc_smem = hb_kv8_tc::Cfg<DH>::FIXED + (p.r.n_segs + 1) * 4;
@@ -523,8 +613,7 @@ int launch(const AttnParams& p, int num_sms, cudaStream_t s, bool pdl, int* laun
   }
   if (rc != HB_OK || p.max_splits == 1) return rc;
   ++*launches;
-  const int cols = static_cast<int>(std::min<long long>(TILE_COLS, cols_bound));
-  return hb_launch_kernel(kv8_join_kernel<DH>, static_cast<unsigned>(p.r.n_segs) * p.r.Hkv * cols, DH, 0, s, true, p, cols);
+  return hb_launch_kernel(kv8_join_kernel<DH>, static_cast<unsigned>(p.r.n_segs) * p.r.Hkv, JOIN_WARPS * 32, 0, s, true, p);
 }
 
 }  // namespace
