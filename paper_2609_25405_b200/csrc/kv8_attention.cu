@@ -30,7 +30,7 @@ constexpr int DEC_WARPS = 4;
 constexpr int DEC_THREADS = DEC_WARPS * 32;
 constexpr int STAGES = 2;   // page blocks of a warp in flight or in use: 16 warps of an SM keep up to 128 KiB
 constexpr int TILE_COLS = 16;
-constexpr int MIN_SPLIT_KEYS = 512, MAX_SPLITS = 128;
+constexpr int MIN_SPLIT_KEYS = 512, MAX_SPLITS = 64;
 constexpr int MAX_SEGS = 8192;
 constexpr uint64_t WAIT_NS = 1000000000ull;
 
@@ -603,7 +603,7 @@ int launch(const AttnParams& p, int num_sms, cudaStream_t s, bool pdl, int* laun
   *launches = 1;
   if (rc == HB_OK && cols_bound > TILE_COLS) {   // segments for the chunk body are possible
     static DynSmemState tc_configured;
-    const int tc_smem = hb_kv8_tc::Cfg<DH>::FIXED + (p.r.n_segs + 1) * 4;
+    const int tc_smem = hb_kv8_tc::Cfg<DH>::FIXED + (p.r.n_segs + 1) * 4 + hb_kv8_tc::MAX_SORTED * 4;
     if (tc_smem > 227 * 1024) return HB_ERR_TOO_LARGE;
     auto tc = hb_kv8_tc::kv8_chunk_kernel<DH>;
     if (hb_ensure_dyn_smem(reinterpret_cast<const void*>(tc), tc_configured, tc_smem) != HB_OK) return HB_ERR_CUDA;

@@ -40,13 +40,14 @@ struct Cfg {
   static constexpr int RAW_OFF = CV * 2 * TILE;
   static constexpr int SC_OFF = RAW_OFF + RAW * RAW_BYTES;   // float2 [CV][PAGES]: factor of the scores, exponent of V
   static constexpr int BAR_OFF = SC_OFF + CV * PAGES * 8;
-  static constexpr int N_BARS = 2 * RAW + 2 * CV + 2 + 2 + 2 + 2;   // raw, cv (full, empty), S full, P ready, Q ready, O full
+  static constexpr int N_BARS = 2 * RAW + 2 * CV + 10;   // raw, cv (full, empty); for A and B: S full, P ready (two halves), Q ready, O full
   static constexpr int MISC_OFF = BAR_OFF + N_BARS * 8;      // abort flag, bad item, tensor-memory base, warp sums
   static constexpr int FIXED = MISC_OFF + 128;
   static constexpr int O_COL = 0, S_COL = 256, Q_COL = 384;
 };
 
-// One lane of the warp issues; the operands are the same in all of them, so that they stay in uniform registers.
+// One lane of the warp issues; the operands are the same in all of them, so that they stay in uniform registers
+// (35 and 67 cycles an instruction at N = 64 and 128, against about 100 from a divergent branch).
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
@@ -62,6 +63,14 @@ __device__ __forceinline__ void commit(uint32_t bar) {
       "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
 
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
 struct TcItem {
   Seg g;
   int seg, head;
@@ -73,6 +82,17 @@ struct TcItem {
 __device__ __forceinline__ int tc_blocks(const Rows& r, const Seg& g) {
   const int cols = g.q_len * r.G;
   return cols > 16 ? (cols + ROWS - 1) / ROWS : 0;
+}
+
+// Items in the order of their cost: with few of them (up to MAX_SORTED blocks of rows, each for all KV heads) a
+// block that got two long ones would be the last by far (84 key tiles where 52 are the mean, in a step of 8
+// chunks over contexts of 0 to 2048).  The blocks take them in rounds, every other round backwards.
+constexpr int MAX_SORTED = 512;
+
+__device__ __forceinline__ int item_of(const uint16_t* order, int total, int n_heads, int round) {
+  const int t = round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+  if (t >= total) return -1;
+  return order ? order[t / n_heads] * n_heads + t % n_heads : t;
 }
 
 __device__ __forceinline__ void tc_item(const Rows& r, const int* prefix, int idx, TcItem& it) {
@@ -101,7 +121,7 @@ kv8_chunk_kernel(const AttnParams p) {
   auto raw_empty = [&](int s) { return bars + 8u * (RAW + s); };
   auto cv_full = [&](int s) { return bars + 8u * (2 * RAW + s); };
   auto cv_empty = [&](int s) { return bars + 8u * (2 * RAW + CV + s); };
-  const uint32_t s_full0 = bars + 8u * (2 * RAW + 2 * CV), p_ready0 = s_full0 + 16u, q_ready0 = p_ready0 + 16u, o_full0 = q_ready0 + 16u;
+  const uint32_t s_full0 = bars + 8u * (2 * RAW + 2 * CV), p_ready0 = s_full0 + 16u, q_ready0 = p_ready0 + 32u, o_full0 = q_ready0 + 16u;
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + C::MISC_OFF);
   volatile int* bad_item = reinterpret_cast<volatile int*>(smem + C::MISC_OFF + 4);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::MISC_OFF + 8);
@@ -117,7 +137,8 @@ kv8_chunk_kernel(const AttnParams p) {
     for (int s = 0; s < CV; ++s) { mbar_init(cv_full(s), 4); mbar_init(cv_empty(s), 1); }
     for (int x = 0; x < 2; ++x) {
       mbar_init(s_full0 + 8u * x, 1);
-      mbar_init(p_ready0 + 8u * x, 4);
+      mbar_init(p_ready0 + 16u * x, 4);
+      mbar_init(p_ready0 + 16u * x + 8u, 4);
       mbar_init(q_ready0 + 8u * x, 4);
       mbar_init(o_full0 + 8u * x, 1);
     }
@@ -130,6 +151,25 @@ kv8_chunk_kernel(const AttnParams p) {
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   const int total = build_prefix<THREADS>(p.r, prefix, warp_sums, [&](const Seg& g) { return tc_blocks(p.r, g) * p.r.Hkv; }, false);
+  const uint16_t* order = nullptr;
+  const int n_blocks = total / p.r.Hkv;
+  if (n_blocks <= MAX_SORTED && total > static_cast<int>(gridDim.x)) {
+    uint16_t* cost = reinterpret_cast<uint16_t*>(prefix + p.r.n_segs + 1);
+    uint16_t* sorted = cost + MAX_SORTED;
+    for (int i = tid; i < n_blocks; i += THREADS) {
+      TcItem it;
+      tc_item(p.r, prefix, i * p.r.Hkv, it);
+      cost[i] = static_cast<uint16_t>(min(65535, max(it.tiles[0], it.tiles[1]) * 2 - (it.tiles[1] == 0)));
+    }
+    __syncthreads();
+    for (int i = tid; i < n_blocks; i += THREADS) {
+      const int mine = cost[i];
+      int rank = 0;
+      for (int k = 0; k < n_blocks; ++k) rank += cost[k] > mine || (cost[k] == mine && k < i);
+      sorted[rank] = static_cast<uint16_t>(i);
+    }
+    order = sorted;
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -139,7 +179,7 @@ kv8_chunk_kernel(const AttnParams p) {
     // ---------------- page blocks ----------------
     uint32_t n = 0;   // tiles asked for so far
     bool ok = true;
-    for (int idx = blockIdx.x; idx < total && ok; idx += gridDim.x) {
+    for (int round = 0, idx; ok && (idx = item_of(order, total, p.r.Hkv, round)) >= 0; ++round) {
       TcItem it;
       tc_item(p.r, prefix, idx, it);
       const int n_pg = (it.key1 + PAGE - 1) / PAGE, n_tiles = (n_pg + PAGES - 1) / PAGES;
@@ -184,7 +224,7 @@ kv8_chunk_kernel(const AttnParams p) {
                idesc_s, ks > 0 ? 1u : 0u);
       commit(s_full0 + 8u * x);
     };
-    for (int idx = blockIdx.x; idx < total && ok; idx += gridDim.x) {
+    for (int round = 0, idx; ok && (idx = item_of(order, total, p.r.Hkv, round)) >= 0; ++round) {
       TcItem it;
       tc_item(p.r, prefix, idx, it);
       const int n_tiles = max(it.tiles[0], it.tiles[1]);
@@ -202,12 +242,16 @@ kv8_chunk_kernel(const AttnParams p) {
         const uint32_t v_tile = base + (n % CV) * 2 * C::TILE + C::TILE;
         for (int x = 0; x < 2 && ok; ++x) {
           if (j < it.tiles[x]) {
-            if (!wait(p_ready0 + 8u * x, n_p[x] & 1u)) break;
-            ++n_p[x];
-            tc_fence_after();
 #pragma unroll
-            for (int ks = 0; ks < BN / 16; ++ks)
+            for (int ks = 0; ks < BN / 16; ++ks) {
+              if (ks % 2 == 0) {   // each half of P has its own barrier
+                if (!wait(p_ready0 + 16u * x + 4u * ks, n_p[x] & 1u)) break;
+                tc_fence_after();
+              }
               mma_ts(tmem + C::O_COL + x * DH, tmem + C::S_COL + x * BN + ks * 8, make_desc(v_tile + ks * 32, 16, 1024), idesc_o, (j > 0 || ks > 0) ? 1u : 0u);
+            }
+            if (!ok) break;
+            ++n_p[x];
             if (j + 1 == it.tiles[x]) commit(o_full0 + 8u * x);
           }
           if (x == 1) commit(cv_empty(n % CV));   // both tiles' reads of this key tile are in front of it
@@ -223,7 +267,7 @@ kv8_chunk_kernel(const AttnParams p) {
     // lanes of a half warp take dimensions whose rows of V^T differ in their swizzle and in their bank of the
     // codes: 0, 3, 4, 7 and 1, 2, 5, 6
     const int i4 = (lane >> 2) & 3, vd = lane < 16 ? (i4 == 0 ? 0 : i4 == 1 ? 3 : i4 == 2 ? 4 : 7) : (i4 == 0 ? 1 : i4 == 1 ? 2 : i4 == 2 ? 5 : 6), vt = lane & 3;
-    for (int idx = blockIdx.x; idx < total && ok; idx += gridDim.x) {
+    for (int round = 0, idx; ok && (idx = item_of(order, total, p.r.Hkv, round)) >= 0; ++round) {
       TcItem it;
       tc_item(p.r, prefix, idx, it);
       const int n_tiles = (it.key1 + BN - 1) / BN;
@@ -291,7 +335,7 @@ kv8_chunk_kernel(const AttnParams p) {
       if (ok && !__all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, WAIT_NS))) ok = false;
       return ok;
     };
-    for (int idx = blockIdx.x; idx < total && ok; idx += gridDim.x) {
+    for (int round = 0, idx; ok && (idx = item_of(order, total, p.r.Hkv, round)) >= 0; ++round) {
       TcItem it;
       tc_item(p.r, prefix, idx, it);
       const int row = x * BM + rr;
@@ -340,11 +384,12 @@ kv8_chunk_kernel(const AttnParams p) {
         float mx = -INFINITY;
 #pragma unroll
         for (int g = 0; g < PAGES; ++g) {
-          float a = -INFINITY, b = -INFINITY;
+          float a = __uint_as_float(sr[g >> 1][(g & 1) * PAGE]), b = __uint_as_float(sr[g >> 1][(g & 1) * PAGE + 1]);
 #pragma unroll
-          for (int i = 0; i < PAGE; i += 2) {
-            a = fmaxf(a, __uint_as_float(sr[(g * PAGE + i) >> 5][(g * PAGE + i) & 31]));
-            b = fmaxf(b, __uint_as_float(sr[(g * PAGE + i + 1) >> 5][(g * PAGE + i + 1) & 31]));
+          for (int i = 2; i < PAGE; i += 4) {   // (three-input maxima)
+            a = fmaxf(fmaxf(a, __uint_as_float(sr[g >> 1][(g & 1) * PAGE + i])), __uint_as_float(sr[g >> 1][(g & 1) * PAGE + i + 1]));
+            if (i + 2 < PAGE)
+              b = fmaxf(fmaxf(b, __uint_as_float(sr[g >> 1][(g & 1) * PAGE + i + 2])), __uint_as_float(sr[g >> 1][(g & 1) * PAGE + i + 3]));
           }
           a = fmaxf(a, b);
           mx = fmaxf(mx, a == -INFINITY ? a : fmaf(a, sc[g].x, sc[g].y));
@@ -369,30 +414,38 @@ kv8_chunk_kernel(const AttnParams p) {
           m = m_new;
         }
         const float neg_m = m == -INFINITY ? 0.0f : -m;
-        uint32_t pk[32];
 #pragma unroll
-        for (int g = 0; g < PAGES; ++g) {
-          const float add = sc[g].y + neg_m;
-          float w[PAGE], sum0 = 0.0f, sum1 = 0.0f;
+        for (int h = 0; h < 2; ++h) {   // two pages, then the other two: the first half of P V starts early
+          uint32_t pk[16];
 #pragma unroll
-          for (int i = 0; i < PAGE; i += 2) {
-            w[i] = ex2_approx(fmaf(__uint_as_float(sr[(g * PAGE + i) >> 5][(g * PAGE + i) & 31]), sc[g].x, add));
-            w[i + 1] = ex2_approx(fmaf(__uint_as_float(sr[(g * PAGE + i + 1) >> 5][(g * PAGE + i + 1) & 31]), sc[g].x, add));
-            sum0 += w[i];
-            sum1 += w[i + 1];
+          for (int g2 = 0; g2 < 2; ++g2) {
+            const int g = h * 2 + g2;
+            const uint64_t mul = pack2(sc[g].x, sc[g].x), add = pack2(sc[g].y + neg_m, sc[g].y + neg_m);
+            float w[PAGE];
+            uint64_t sum[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < PAGE; i += 2) {
+              float u, v;
+              unpack2(fma2(pack2(__uint_as_float(sr[h][g2 * PAGE + i]), __uint_as_float(sr[h][g2 * PAGE + i + 1])), mul, add), u, v);
+              w[i] = ex2_approx(u);
+              w[i + 1] = ex2_approx(v);
+              sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pack2(w[i], w[i + 1]));
+            }
+            float u, v;
+            unpack2(add2(sum[0], sum[1]), u, v);
+            l = fmaf(u + v, pow2f(max(-126, min(126, static_cast<int>(-sc[g].y)))), l);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {   // the order of the keys in V^T's rows: 2t, 2t+1, 2t+8, 2t+9
+              pk[g2 * 8 + 2 * t] = pack_half2(w[2 * t], w[2 * t + 1]);
+              pk[g2 * 8 + 2 * t + 1] = pack_half2(w[2 * t + 8], w[2 * t + 9]);
+            }
           }
-          l = fmaf(sum0 + sum1, pow2f(max(-126, min(126, static_cast<int>(-sc[g].y)))), l);
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {   // the order of the keys in V^T's rows: 2t, 2t+1, 2t+8, 2t+9
-            pk[g * 8 + 2 * t] = pack_half2(w[2 * t], w[2 * t + 1]);
-            pk[g * 8 + 2 * t + 1] = pack_half2(w[2 * t + 8], w[2 * t + 9]);
-          }
+          tmem_st16(t_s + h * 16, pk);
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_ready0 + 16u * x + 8u * h);
         }
-        tmem_st32(t_s, pk);
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_ready0 + 8u * x);
       }
       n += all_tiles;
       if (n_tiles > 0 && wait(o_full0 + 8u * x, n_o & 1u)) {
