@@ -62,6 +62,22 @@ __device__ __forceinline__ void e4m3x4_to_half2x2(uint32_t w, uint32_t& lo, uint
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
       : "=r"(lo), "=r"(hi) : "r"(w));
 }
+// NaN in V.  A weight of zero does not keep a NaN out of a sum, so where a page holds keys that some rows must not
+// see, NaN codes are replaced by zero and the rows that do see such a token become NaN as a whole (elsewhere
+// NaN takes its way through the sum, into its own dimensions).
+// Zeroes the NaN codes (0x7f, 0xff) of a word; returns a bit (the lowest) for each of its bytes that was one.
+__device__ __forceinline__ uint32_t drop_nan(uint32_t& w) {
+  const uint32_t bits = (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u;
+  w &= ~(bits * 0xffu);
+  return bits;
+}
+// The tokens of a page that the warp's lanes have found NaN in: bytes are tokens 2t, 2t+1, 2t+8, 2t+9; every lane gets bit
+// `token` for each.
+__device__ __forceinline__ uint32_t nan_tokens(uint32_t bytes, int t) {
+  const uint32_t mine = ((bytes & 1u) | ((bytes >> 7) & 2u)) << (2 * t) | (((bytes >> 16) & 1u) | ((bytes >> 23) & 2u)) << (2 * t + 8);
+  return __reduce_or_sync(0xffffffffu, mine);
+}
+
 // Two floats -> two codes (first in the low byte): round to nearest even, saturating, NaN stays NaN.
 __device__ __forceinline__ uint32_t floats_to_e4m3x2(float a, float b) {
   uint32_t r;

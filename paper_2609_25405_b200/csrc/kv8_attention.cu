@@ -218,6 +218,24 @@ __device__ __forceinline__ void begin(const AttnParams& p, const Item& it, State
   }
 }
 
+// Replaces the NaN codes of a page's V by zero, in shared memory; returns a bit for each token that had one.  The warp.
+template <int DH>
+__device__ __noinline__ uint32_t drop_nan_page(uint32_t blk) {
+  const int lane = threadIdx.x & 31;
+  uint32_t bytes = 0;
+#pragma unroll 1
+  for (int c = 0; c < DH / 32; ++c) {
+    const uint32_t at = blk + Block<DH>::V_OFF + c * 512 + lane * 16;
+    uint4 v = lds128(at);
+    const uint32_t here = drop_nan(v.x) | drop_nan(v.y) | drop_nan(v.z) | drop_nan(v.w);
+    if (here) asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    bytes |= here;
+  }
+  bytes = nan_tokens(bytes, lane & 3);
+  if (bytes) fence_async_smem();   // the next copy into this stage comes behind these stores
+  return bytes;
+}
+
 // One page (16 keys from `key`) out of shared memory at `blk`.
 template <int DH, int NT>
 __device__ __forceinline__ void page_step(const AttnParams& p, const Item& it, uint32_t blk, int key, State<DH, NT>& st) {
@@ -291,6 +309,19 @@ __device__ __forceinline__ void page_step(const AttnParams& p, const Item& it, u
         st.o[nt][mt][0] *= f[0]; st.o[nt][mt][1] *= f[1];
         st.o[nt][mt][2] *= f[0]; st.o[nt][mt][3] *= f[1];
       }
+    }
+  }
+  // a page that reaches behind what the first row sees, in a segment of several rows: NaN codes of V go (in place)
+  if (key + PAGE - 1 > it.g.pos_start && it.g.q_len > 1) {
+    const uint32_t nan_at = drop_nan_page<DH>(blk);
+    if (nan_at) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int last = min(st.lim[nt][e] - key, PAGE - 1);   // the column sees tokens 0 .. last of the page
+          if (last >= 0 && (nan_at & ((2u << last) - 1u))) st.l[nt][e] = __uint_as_float(0x7fc00000u);
+        }
     }
   }
   uint32_t pt[NT][2];

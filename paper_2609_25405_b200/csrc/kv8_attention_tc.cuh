@@ -39,7 +39,8 @@ struct Cfg {
   static constexpr int RAW_BYTES = PAGES * Block<DH>::BYTES;
   static constexpr int RAW_OFF = CV * 2 * TILE;
   static constexpr int SC_OFF = RAW_OFF + RAW * RAW_BYTES;   // float2 [CV][PAGES]: factor of the scores, exponent of V
-  static constexpr int BAR_OFF = SC_OFF + CV * PAGES * 8;
+  static constexpr int NAN_OFF = SC_OFF + CV * PAGES * 8;    // uint32 [CV][PAGES]: tokens whose V holds NaN (see nan_tokens)
+  static constexpr int BAR_OFF = NAN_OFF + CV * PAGES * 4;
   static constexpr int N_BARS = 2 * RAW + 2 * CV + 10;   // raw, cv (full, empty); for A and B: S full, P ready (two halves), Q ready, O full
   static constexpr int MISC_OFF = BAR_OFF + N_BARS * 8;      // abort flag, bad item, tensor-memory base, warp sums
   static constexpr int FIXED = MISC_OFF + 128;
@@ -77,6 +78,7 @@ struct TcItem {
   int row0, n_rows;      // rows [row0, row0 + n_rows) of the segment's q_len * G
   int tiles[2];          // key tiles of A and of B (0: no rows)
   int key1;              // keys the item needs (those of its last row)
+  int all_see;           // last key that all of its rows see
 };
 
 __device__ __forceinline__ int tc_blocks(const Rows& r, const Seg& g) {
@@ -106,13 +108,15 @@ __device__ __forceinline__ void tc_item(const Rows& r, const int* prefix, int id
   const int last_a = min(it.n_rows, BM) - 1;
   it.tiles[0] = (it.g.pos_start + (it.row0 + last_a) / r.G + 1 + BN - 1) / BN;
   it.key1 = it.g.pos_start + (it.row0 + it.n_rows - 1) / r.G + 1;
+  it.all_see = it.g.pos_start + it.row0 / r.G;
   it.tiles[1] = it.n_rows > BM ? (it.key1 + BN - 1) / BN : 0;
 }
 
 template <int DH>
 __global__ void __launch_bounds__(THREADS, 1)
 kv8_chunk_kernel(const AttnParams p) {
-  grid_dep_wait();
+  // Launched behind the decode kernel, whose blocks have all waited for what was before them; it reads nothing of
+  // that kernel's, so it takes an SM as soon as the decode blocks there are done, and waits for the rest at its end.
   using C = Cfg<DH>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -129,9 +133,10 @@ kv8_chunk_kernel(const AttnParams p) {
   int* prefix = reinterpret_cast<int*>(smem + C::FIXED);
   if (base & 1023u) {   // the swizzled tiles need it; the same in every thread
     if (tid == 0) atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
-    grid_dep_launch();
+    grid_dep_wait();
     return;
   }
+  grid_dep_launch();   // (what follows waits for this kernel's end)
   if (tid == 0) {
     for (int s = 0; s < RAW; ++s) { mbar_init(raw_full(s), 1); mbar_init(raw_empty(s), 4); }
     for (int s = 0; s < CV; ++s) { mbar_init(cv_full(s), 4); mbar_init(cv_empty(s), 1); }
@@ -286,6 +291,8 @@ kv8_chunk_kernel(const AttnParams p) {
           sc.y = static_cast<float>(exponent_of(sc.y));
         }
         if (lane == 0) *reinterpret_cast<float2*>(smem + C::SC_OFF + (cs * PAGES + pg) * 8) = sc;
+        const bool hidden = key + PAGE - 1 > it.all_see;   // some rows must not see all of this page
+        uint32_t nan_bytes = 0;
 #pragma unroll
         for (int i = 0; i < DH / 32; ++i) {
           const int hf = i >> 1, u = (i & 1) * 32 + lane, tok = u >> 2, q = u & 3;
@@ -308,7 +315,11 @@ kv8_chunk_kernel(const AttnParams p) {
 #pragma unroll
         for (int c = 0; c < DH / 32; ++c) {
           const uint4 v = lds128(src + Block<DH>::V_OFF + c * 512 + (vd * 4 + vt) * 16);
-          const uint32_t w[4] = {v.x & keep, v.y & keep, v.z & keep, v.w & keep};
+          uint32_t w[4] = {v.x & keep, v.y & keep, v.z & keep, v.w & keep};
+          if (hidden) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) nan_bytes |= drop_nan(w[e]);
+          }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             uint2 h;
@@ -316,6 +327,8 @@ kv8_chunk_kernel(const AttnParams p) {
             *reinterpret_cast<uint2*>(v_tile + (c * 32 + e * 8 + vd) * 128 + (((pg * 2 + (vt >> 1)) ^ vd) << 4) + (vt & 1) * 8) = h;
           }
         }
+        if (hidden) nan_bytes = nan_tokens(nan_bytes, vt);
+        if (lane == 0) *reinterpret_cast<uint32_t*>(smem + C::NAN_OFF + (cs * PAGES + pg) * 4) = nan_bytes;
         fence_async_smem();
         __syncwarp();
         if (lane == 0) {
@@ -375,6 +388,15 @@ kv8_chunk_kernel(const AttnParams p) {
         for (int g = 0; g < PAGES; ++g) sc[g] = *reinterpret_cast<const float2*>(smem + C::SC_OFF + (((n + j) % CV) * PAGES + g) * 8);
         tmem_ld_wait();
         const int key = j * BN;
+        if (key + BN - 1 > it.all_see) {   // NaN codes of V were dropped where some row must not see them
+          bool sees_nan = false;
+#pragma unroll
+          for (int g = 0; g < PAGES; ++g) {
+            const int last = min(pos - key - g * PAGE, PAGE - 1);   // the row sees tokens 0 .. last of the page
+            if (last >= 0) sees_nan |= (*reinterpret_cast<const uint32_t*>(smem + C::NAN_OFF + (((n + j) % CV) * PAGES + g) * 4) & ((2u << last) - 1u)) != 0;
+          }
+          if (sees_nan) l = __uint_as_float(0x7fc00000u);
+        }
         if (key + BN - 1 > pos) {   // the diagonal, or rows of nobody
           const int last = pos - key;
 #pragma unroll
@@ -487,7 +509,7 @@ kv8_chunk_kernel(const AttnParams p) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
-  grid_dep_launch();
+  grid_dep_wait();
 }
 
 }  // namespace hb_kv8_tc

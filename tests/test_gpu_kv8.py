@@ -297,6 +297,40 @@ def test_stale_bytes_behind_the_last_key():
     _check_attend(ctx, kv, 0, rows, 8, 2, 128, 6)
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+def test_nan_in_tokens_that_come_later(dh):
+    """A token whose key and value (or value alone, in one dimension) are NaN: rows before it are what they are without it,
+    to the bit; rows that see it are NaN (in that dimension at least); in decode rows, small and large chunks."""
+    cfg, ctx = context(8, 2, dh)
+    segs = [(20, 4), (600, 2), (9, 40), (100, 200), (30, 1), (70, 130)]
+    bad = [22, 601, 30, 250, 7, 70 + 129]               # position of the token in its request
+    rows = Rows(segs, 120, seed=5)
+    kv = random_arena(cfg, 120, 4)
+    q = torch.randn(rows.T, 8 * dh, device="cuda").half()
+    clean = torch.empty_like(q)
+    ctx.kv8_attention(kv, 0, rows.dev, q, clean)
+    saved = kv.arena.clone()
+    for whole in (True, False):
+        a = layer_bytes(kv, 0).copy()
+        for pages, b in zip(rows.pages, bad):
+            dims = np.arange(dh) if whole else np.array([dh // 2 + 3])
+            blk = a[pages[b // 16]]
+            blk[:, 16 * dh + O.v_byte(b % 16, dims)] = 0x7F
+            if whole:
+                blk[:, O.k_byte(b % 16, dims)] = 0xFF
+        kv.arena[:a.size] = torch.from_numpy(a.reshape(-1)).cuda()
+        out = torch.empty_like(q)
+        ctx.kv8_attention(kv, 0, rows.dev, q, out)
+        assert ctx.status_poll() == 0
+        for (p, n), at, b in zip(segs, rows.start, bad):
+            sees = torch.arange(p, p + n, device="cuda") >= b
+            got, ref = out[at:at + n].view(n, 8, dh), clean[at:at + n].view(n, 8, dh)
+            assert torch.equal(got[~sees], ref[~sees]), (p, n)
+            hit = got[sees] if whole else got[sees][..., dh // 2 + 3]
+            assert bool(torch.isnan(hit).all()), (p, n)
+        kv.arena.copy_(saved)
+
+
 def test_a_requests_result_does_not_depend_on_its_batch():
     """Every segment alone gives the bits it gives in the batch."""
     cfg, ctx = context(32, 8, 128)
