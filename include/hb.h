@@ -505,8 +505,10 @@ HB_API int hb_kv8_create(const hb_model_cfg* cfg, void* arena, size_t arena_byte
  * pt_start and pt_len are read (the other fields are not).  Unlike in hb_batch_desc, segments need
  * not be adjacent and q_len may be 0; rows whose row_seg is -1 belong to nobody (padding): what
  * the calls write for rows is left untouched there.  Nothing is read on the host, so a captured
- * call sees what the arrays hold when it is replayed.  The two bounds size the launches: a segment
- * beyond one of them, a page id outside the arena, or any other inconsistent field is reported
+ * call sees what the arrays hold when it is replayed.  row_seg[r] = s exactly for the rows of
+ * segment s, and no row belongs to two segments.  Limits (HB_ERR_TOO_LARGE beyond them): 8192
+ * segments, 2^26 rows, max_keys 2^30.  The two bounds size the launches: a segment beyond one of
+ * them, a page id outside the arena, or any other inconsistent field is reported
  * through the status word (HB_STATUS_APPEND_INDEX / HB_STATUS_ATTN_INDEX) and skipped. */
 typedef struct {
   const hb_seg* segs;        /* device [n_segs], 16-byte aligned                        */
@@ -551,9 +553,12 @@ HB_API int hb_kv8_append(hb_ctx* ctx, hb_kv* kv, int32_t layer, const hb_rows* r
  *   workspace  device, 256-byte aligned, hb_kv8_attention_workspace bytes for these rows; needs no
  *        initialisation and belongs to the call until it has run: calls that may run at the same
  *        time need a workspace each
- * Scores, softmax and sums in fp32, probabilities rounded to fp16 for the tensor cores.  How a
- * segment's keys are split depends on its own lengths only, never on the rest of the batch.  (Inside
- * hb_mixed_step the splits may be longer: there the context's limits choose them.) */
+ * Scores, softmax and sums in fp32, probabilities rounded to fp16 for the tensor cores.  A NaN in
+ * a key makes the rows that see it NaN; a NaN in a value makes at least that dimension of them NaN
+ * (the whole row where other rows of the segment come before the token).  Rows before the token
+ * are not touched by it.  How a segment's keys are split depends on its own lengths only, never on
+ * the rest of the batch.  (Inside hb_mixed_step the splits may be longer: there the context's limits
+ * choose them.) */
 HB_API int hb_kv8_attention_workspace(const hb_model_cfg* cfg, const hb_rows* rows, size_t* out_bytes);
 HB_API int hb_kv8_attention(hb_ctx* ctx, hb_kv* kv, int32_t layer, const hb_rows* rows, const void* q, int64_t q_stride,
                      void* out, int64_t out_stride, float scale, void* workspace, size_t workspace_bytes, void* stream);

@@ -564,13 +564,16 @@ namespace {
 
 bool same_cfg(const hb_model_cfg& a, const hb_model_cfg& b) { return memcmp(&a, &b, sizeof(hb_model_cfg)) == 0; }
 
+// Sizes whose products the kernels hold in 32 bits (rows x heads of a group, keys rounded up, items).
+bool kv8_limits_ok(const hb_rows& r) { return r.n_segs <= hb_kv8_max_segs() && r.n_rows <= (1 << 26) && r.max_keys <= (1 << 30); }
+
 // What both operators check of the cache, the layer and the rows, and the kernels' view of them.
 int kv8_rows(hb_ctx* c, hb_kv* kv, int32_t layer, const hb_rows* r, hb_kv8::Rows* out) {
   if (!c || !kv || !r) return HB_ERR_BAD_ARG;
   if (!kv->e4m3 || !kv->arena || !same_cfg(kv->cfg, c->cfg)) return HB_ERR_BAD_ARG;
   if (layer < 0 || layer >= c->cfg.n_layers) return HB_ERR_BAD_ARG;
   if (r->n_segs < 0 || r->n_page_ids < 0 || r->n_rows < 0 || r->max_q_len < 0 || r->max_keys < 0) return HB_ERR_BAD_ARG;
-  if (r->n_segs > hb_kv8_max_segs()) return HB_ERR_TOO_LARGE;
+  if (!kv8_limits_ok(*r)) return HB_ERR_TOO_LARGE;
   if ((r->n_segs > 0 && !r->segs) || (r->n_page_ids > 0 && !r->page_ids) || (r->n_rows > 0 && !r->row_seg)) return HB_ERR_BAD_ARG;
   if (misaligned(r->segs, 16) || misaligned(r->page_ids, 4) || misaligned(r->row_seg, 4)) return HB_ERR_BAD_ARG;
   int dev = -1;
@@ -619,7 +622,7 @@ int hb_kv8_append(hb_ctx* c, hb_kv* kv, int32_t layer, const hb_rows* rows, cons
 
 int hb_kv8_attention_workspace(const hb_model_cfg* cfg, const hb_rows* rows, size_t* out_bytes) {
   if (!cfg_ok(cfg) || !rows || !out_bytes || rows->n_rows < 0 || rows->n_segs < 0 || rows->max_keys < 0) return HB_ERR_BAD_ARG;
-  if (rows->n_segs > hb_kv8_max_segs()) return HB_ERR_TOO_LARGE;
+  if (!kv8_limits_ok(*rows)) return HB_ERR_TOO_LARGE;
   *out_bytes = hb_kv8_attention_scratch(*cfg, rows->n_rows, rows->n_segs, rows->max_keys, hb_kv8_min_split_keys());
   return HB_OK;
 }

@@ -459,9 +459,10 @@ def test_refusals():
         r = B.RowsStruct.from_buffer_copy(rows.dev.struct)
         setattr(r, k, v)
         assert attend(r=r) == -1, k
-    r = B.RowsStruct.from_buffer_copy(rows.dev.struct)
-    r.n_segs = 8193
-    assert attend(r=r) == -5
+    for k, v in (("n_segs", 8193), ("n_rows", (1 << 26) + 1), ("max_keys", (1 << 30) + 1)):
+        r = B.RowsStruct.from_buffer_copy(rows.dev.struct)
+        setattr(r, k, v)
+        assert attend(r=r) == -5, k
 
     def append(**kw):
         a = B.AppendArgs(qkv=qp, q_out=qp, qkv_stride=768, q_stride=512, norm_eps=1e-6, rope_rows=0, rot_dim=0, rope_layout=0)

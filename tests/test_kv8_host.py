@@ -80,6 +80,7 @@ def test_workspace_grows_with_the_splits():
     assert size(1000, 4, 1024) == (0, 4 * TINY.Hkv * 16 * 3 * rec)     # ... or 16 columns per segment and KV head
     assert size(4, 4, 1 << 20) == (0, 4 * TINY.Hq * 64 * rec)          # never more than 64 splits
     assert size(-1, 1, 10)[0] == -1 and size(1, -1, 10)[0] == -1 and size(1, 1, -1)[0] == -1 and size(1, 8193, 10)[0] == -5
+    assert size((1 << 26) + 1, 1, 10)[0] == -5 and size(1, 1, (1 << 30) + 1)[0] == -5
 
 
 def test_calls_without_a_context_or_cache_are_refused():
