@@ -537,9 +537,12 @@ class Rope:
 
     def __init__(self, cos, sin, layout=ROPE_PAIRS):
         for t in (cos, sin):
-            if t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous() or t.dim() != 2 or t.shape != cos.shape:
+            if t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous() or t.dim() != 2 or t.shape != cos.shape or \
+                    t.device != cos.device:
                 raise ValueError("cos / sin: contiguous fp32 tensors [positions, rot_dim / 2] on the GPU")
         self.cos, self.sin, self.layout = cos, sin, layout
+        self.index = cos.get_device()
+        self.fields = (cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], layout)
 
     @classmethod
     def table(cls, n_pos, rot_dim, theta, layout=ROPE_PAIRS, scaling=None, device="cuda"):
@@ -727,27 +730,30 @@ class Context:
             raise ValueError(f"rows and cache on the context's device, {self.device}")
         return self.index
 
+    def _head_gain(self, gain, name):
+        if gain is None:
+            return None
+        if gain.dtype is not torch.bfloat16 or gain.get_device() != self.index or gain.shape != (self.cfg.head_dim,) or \
+                not gain.is_contiguous():
+            raise ValueError(f"{name}: a contiguous bf16 tensor [{self.cfg.head_dim}] on {self.device}")
+        return gain.data_ptr()
+
     def kv8_append(self, kv, layer, rows, qkv, q_out, rope=None, q_norm=None, k_norm=None, norm_eps=1e-6, stream=None):
         """hb_kv8_append: head norms (bf16 gains [Dh] or None), rotation (Rope or None), K / V of every row of
         `rows` (SegRows) appended to layer `layer` of a KvCache8; qkv fp16 [T, (Hq + 2 Hkv) Dh], q_out
         fp16 [T, Hq Dh] (rows may be strided views)."""
         c = self.cfg
         T, dev = rows.struct.n_rows, self._same_device(rows, kv)
-        a = AppendArgs()
-        a.qkv, a.qkv_stride = _rows_f16(qkv, T, (c.n_heads + 2 * c.n_kv_heads) * c.head_dim, dev, "qkv")
-        a.q_out, a.q_stride = _rows_f16(q_out, T, c.n_heads * c.head_dim, dev, "q_out")
-        for gain, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-            if gain is not None and (gain.dtype != torch.bfloat16 or gain.get_device() != dev or gain.shape != (c.head_dim,) or
-                                     not gain.is_contiguous()):
-                raise ValueError(f"{name}: a bf16 tensor [{c.head_dim}] on cuda:{dev}")
-        a.q_gain = q_norm.data_ptr() if q_norm is not None else None
-        a.k_gain = k_norm.data_ptr() if k_norm is not None else None
-        a.norm_eps = norm_eps
+        xp, xs = _rows_f16(qkv, T, (c.n_heads + 2 * c.n_kv_heads) * c.head_dim, dev, "qkv")
+        qp, qs = _rows_f16(q_out, T, c.n_heads * c.head_dim, dev, "q_out")
+        cos = sin = None
+        n_pos = rot = layout = 0
         if rope is not None:
-            if rope.cos.get_device() != dev:
+            if rope.index != dev:
                 raise ValueError(f"rope: tables on cuda:{dev}")
-            a.rope_cos, a.rope_sin = rope.cos.data_ptr(), rope.sin.data_ptr()
-            a.rope_rows, a.rot_dim, a.rope_layout = rope.cos.shape[0], 2 * rope.cos.shape[1], rope.layout
+            cos, sin, n_pos, rot, layout = rope.fields
+        a = AppendArgs(xp, qp, xs, qs, self._head_gain(q_norm, "q_norm"), self._head_gain(k_norm, "k_norm"), norm_eps, cos, sin,
+                       n_pos, rot, layout)
         rc = lib.hb_kv8_append(self.handle, kv.handle, layer, C.byref(rows.struct), C.byref(a), _stream_of(stream, dev))
         if rc != HB_OK:
             raise HbError(rc, "hb_kv8_append")
