@@ -31,6 +31,10 @@ constexpr int THREADS = 448;
 constexpr int BM = 128, ROWS = 2 * BM;   // rows of a tile, of an item
 constexpr int BN = 64, PAGES = BN / PAGE;
 constexpr int RAW = 3, CV = 3;           // stages of the ring of codes, of converted tiles
+// Items with a bad page, by round.  The copies run ahead of an item's last store by at most RAW + CV + 1 key tiles, so
+// by no more items: a slot is not used again before it has been read.
+constexpr int BAD = 8;
+static_assert(BAD > RAW + CV + 1 && (BAD & (BAD - 1)) == 0, "slots of bad items");
 constexpr uint64_t WAIT_NS = 1000000000ull;
 
 template <int DH>
@@ -42,8 +46,8 @@ struct Cfg {
   static constexpr int NAN_OFF = SC_OFF + CV * PAGES * 8;    // uint32 [CV][PAGES]: tokens whose V holds NaN (see nan_tokens)
   static constexpr int BAR_OFF = NAN_OFF + CV * PAGES * 4;
   static constexpr int N_BARS = 2 * RAW + 2 * CV + 10;   // raw, cv (full, empty); for A and B: S full, P ready (two halves), Q ready, O full
-  static constexpr int MISC_OFF = BAR_OFF + N_BARS * 8;      // abort flag, bad item, tensor-memory base, warp sums
-  static constexpr int FIXED = MISC_OFF + 128;
+  static constexpr int MISC_OFF = BAR_OFF + N_BARS * 8;      // abort flag, tensor-memory base, warp sums, bad items
+  static constexpr int FIXED = MISC_OFF + 128 + BAD * 4;
   static constexpr int O_COL = 0, S_COL = 256, Q_COL = 384;
 };
 
@@ -127,7 +131,7 @@ kv8_chunk_kernel(const AttnParams p) {
   auto cv_empty = [&](int s) { return bars + 8u * (2 * RAW + CV + s); };
   const uint32_t s_full0 = bars + 8u * (2 * RAW + 2 * CV), p_ready0 = s_full0 + 16u, q_ready0 = p_ready0 + 32u, o_full0 = q_ready0 + 16u;
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + C::MISC_OFF);
-  volatile int* bad_item = reinterpret_cast<volatile int*>(smem + C::MISC_OFF + 4);
+  volatile int* bad_items = reinterpret_cast<volatile int*>(smem + C::MISC_OFF + 128);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::MISC_OFF + 8);
   int* warp_sums = reinterpret_cast<int*>(smem + C::MISC_OFF + 64);
   int* prefix = reinterpret_cast<int*>(smem + C::FIXED);
@@ -148,7 +152,7 @@ kv8_chunk_kernel(const AttnParams p) {
       mbar_init(o_full0 + 8u * x, 1);
     }
     *abort_flag = 0u;
-    *bad_item = -1;
+    for (int i = 0; i < BAD; ++i) bad_items[i] = -1;
     mbar_init_fence();
   }
   if (warp == 1) {
@@ -196,7 +200,7 @@ kv8_chunk_kernel(const AttnParams p) {
           const bool bad = have + lane < n_pg && (cur < 0 || cur >= p.r.n_pages);
           if (bad) {   // reported; the item runs on another page and its rows are not stored
             atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
-            *bad_item = idx;
+            bad_items[round & (BAD - 1)] = idx;
             cur = 0;
           }
           have += 32;
@@ -474,7 +478,7 @@ kv8_chunk_kernel(const AttnParams p) {
         ++n_o;
         tc_fence_after();
         const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-        const bool store = valid && *bad_item != idx;
+        const bool store = valid && bad_items[round & (BAD - 1)] != idx;
         __half* dst = p.out + tok * p.out_stride + head * DH;
 #pragma unroll 1
         for (int c = 0; c < DH; c += 32) {

@@ -350,6 +350,27 @@ def test_a_requests_result_does_not_depend_on_its_batch():
     assert ctx.status_poll() == 0
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+def test_as_many_segments_as_there_may_be(dh):
+    """8192 segments, most of them without rows: chunks and decode rows among them give the bits they give alone."""
+    cfg, ctx = context(8, 2, dh)
+    kv = random_arena(cfg, 300, 4)
+    some = {0: (40, 70), 3000: (300, 1), 5001: (0, 33), 8191: (500, 300)}
+    segs = [some.get(i, (0, 0)) for i in range(8192)]
+    rows = Rows(segs, 300, seed=3)
+    q = torch.randn(rows.T, 8 * dh, device="cuda").half()
+    out = torch.empty_like(q)
+    ctx.kv8_attention(kv, 0, rows.dev, q, out)
+    for i, (p, n) in some.items():
+        one = Rows([(p, n)], 300)
+        one.dev.page_ids.copy_(torch.from_numpy(rows.pages[i]).cuda())
+        at = rows.start[i]
+        alone = torch.empty(n, 8 * dh, dtype=torch.float16, device="cuda")
+        ctx.kv8_attention(kv, 0, one.dev, q[at:at + n].contiguous(), alone)
+        assert torch.equal(alone, out[at:at + n]), (p, n)
+    assert ctx.status_poll() == 0
+
+
 def test_long_contexts_and_offsets_beyond_32_bits():
     """An arena of more than 4 GiB, contexts of 40000 and 131072 keys whose pages lie at its far end (listed
     several times over), appended to and read."""
@@ -426,6 +447,31 @@ def test_bad_page_ids_and_segments_are_reported_and_skipped():
     ids[2 + 43] = -7                                   # the page row 1 writes (position 700, page 43 of segment 1)
     ctx.kv8_append(kv, 0, B.SegRows(rows.dev.segs, ids, rows.dev.row_seg, 20, 701), x, torch.empty_like(q))
     assert ctx.status_poll() == 4
+
+
+def test_many_chunks_with_bad_pages():
+    """Short chunks, two out of three of them with a page id outside the arena, several of those in a row for every
+    block: none of their rows is written, all others are right."""
+    cfg, ctx = context(8, 2, 64)
+    kv = random_arena(cfg, 1100, 5)
+    segs = [(i % 23, 5 + i % 12) for i in range(500)]  # 20 to 64 columns, one or two pages
+    rows = Rows(segs, 1100, seed=6)
+    q = torch.randn(rows.T, 8 * 64, device="cuda").half()
+    good = torch.empty_like(q)
+    ctx.kv8_attention(kv, 0, rows.dev, q, good)
+    assert ctx.status_poll() == 0
+    ids = rows.dev.page_ids.clone()
+    bad = [i for i in range(500) if i // 150 % 3 != 1 and i % 7 < 5]
+    first = rows.table[:, 4]
+    ids[torch.from_numpy(first[bad]).long().cuda()] = 1100
+    out = torch.full_like(q, -3.0)
+    ctx.kv8_attention(kv, 0, B.SegRows(rows.dev.segs, ids, rows.dev.row_seg, 16, 38), q, out)
+    assert ctx.status_poll() == 2
+    gone = np.zeros(rows.T, dtype=bool)
+    for i in bad:
+        gone[rows.start[i]:rows.start[i] + segs[i][1]] = True
+    gone = torch.from_numpy(gone).cuda()
+    assert torch.all(out[gone] == -3.0) and torch.equal(out[~gone], good[~gone])
 
 
 def test_append_beyond_the_rotary_table_is_reported():
