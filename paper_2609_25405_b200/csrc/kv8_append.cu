@@ -12,12 +12,16 @@
 // share a row, 8 dimensions each: 16-byte loads; the rotary partner (i + rot_dim / 2) sits at the same place of
 // another lane.
 //   All segments of up to SMALL_ROWS rows (decode): a warp per row and task, in one wave of blocks; a row that
-//     does not lead has no key / value task.  Latency decides: 64 rows of the 7B shape 3.5 us.
+//     does not lead has no key / value task.  Latency decides: 64 rows of the 7B shape 3.2 us.
 //   Otherwise resident blocks walk over two kinds of tasks.  A page with more than SMALL_ROWS new rows is a
 //     block's: each of the four warps has four of its slots, w has 2w, 2w + 1, 2w + 8, 2w + 9, the tokens of
 //     whole words of V, so that a page that starts afresh is written in words out of registers.  SHARE tasks
 //     look at the same 16 rows, find such leaders and share what they have to do (looking costs two
 //     dependent loads, so few look).  A page with fewer new rows goes to the query warps of its leader.
+//     4096 rows in 8 chunks, 32 / 8 heads of 128, norms and halves: 46 us = 2.1 TB/s (33 us without norms, in pairs).  No
+//     unit is full (issue slots 45 %): the chain row, segment, page id, old scale and the rows themselves decides, with
+//     the 16 warps per SM that 128 registers allow.  All loads of a query task ahead of its look-up: 51 us (spills);
+//     four of them: 47.
 #include <algorithm>
 
 #include "kv8.cuh"

@@ -12,7 +12,10 @@
 // are the same.  With a slice at hand the CTA passes over it three times: its maximum (while the chunks
 // arrive), the two sums relative to that maximum, the logits that can be alternatives.  Then the next
 // slice's chunks are asked for.  Bound by HBM for many rows: three CTAs per SM keep up to 192 KiB in
-// flight; the instructions (about 7 per logit, of them one exponential on the 16-per-clock unit) stay below.
+// flight and overlap each other's loads, sums and selections.  400 rows of 128256 in fp32: 39 us = 5.3 TB/s without
+// alternatives, 54 us with 20 (about 20 instructions per logit in all, issue slots 59 % busy).  2048 rows of 32000 in
+// fp16: 33 us = 4.0 TB/s; there the one exponential per logit on the 16-per-clock unit takes 15 of them.  One
+// row of 128256 takes 8.3 us: a cluster of 8, one slice each, and the join.
 //
 // Alternatives are compared as 64-bit keys: the logit's bits made orderable, then the complement of its
 // index, so that all keys differ, equal logits rank by index, and nothing depends on the order in which
