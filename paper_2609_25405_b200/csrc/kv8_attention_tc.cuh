@@ -148,7 +148,6 @@ kv8_chunk_kernel(const AttnParams p) {
     grid_dep_wait();
     return;
   }
-  grid_dep_launch();   // (what follows waits for this kernel's end)
   if (tid == 0) {
     for (int s = 0; s < RAW; ++s) { mbar_init(raw_full(s), 1); mbar_init(raw_empty(s), 4); }
     for (int s = 0; s < CV; ++s) { mbar_init(cv_full(s), 4); mbar_init(cv_empty(s), 1); }
@@ -191,6 +190,9 @@ kv8_chunk_kernel(const AttnParams p) {
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  // What follows waits for this kernel's end.  It may start only now that every block has its tensor memory: a block of a
+  // later kernel that held some while it waited would keep a block here from starting.
+  grid_dep_launch();
 
   if (warp == 0) {
     // ---------------- page blocks ----------------
