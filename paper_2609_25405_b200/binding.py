@@ -509,13 +509,13 @@ class SegRows:
             raise ValueError("segs [R, 12], page_ids [n], row_seg [T]")
         self.segs, self.page_ids, self.row_seg = segs, page_ids, row_seg
         self.index = segs.get_device()
-        self._need = {}            # workspace bytes by (n_kv_heads, head_dim)
+        self._need = {}            # workspace bytes by (n_heads, n_kv_heads, head_dim)
         self.struct = RowsStruct(segs.data_ptr(), page_ids.data_ptr(), row_seg.data_ptr(), segs.shape[0],
                                  page_ids.shape[0], row_seg.shape[0], int(max_q_len), int(max_keys))
 
     def workspace_bytes(self, cfg):
         """hb_kv8_attention_workspace of these rows."""
-        key = (cfg.n_kv_heads, cfg.head_dim)
+        key = (cfg.n_heads, cfg.n_kv_heads, cfg.head_dim)
         if key not in self._need:
             need = C.c_size_t()
             check(lib.hb_kv8_attention_workspace(C.byref(cfg), C.byref(self.struct), C.byref(need)), "hb_kv8_attention_workspace")

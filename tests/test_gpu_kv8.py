@@ -474,6 +474,19 @@ def test_many_chunks_with_bad_pages():
     assert torch.all(out[gone] == -3.0) and torch.equal(out[~gone], good[~gone])
 
 
+def test_rows_of_one_step_for_two_models():
+    """The same SegRows in contexts that differ in their query heads only: each call has the workspace it needs."""
+    rows = Rows([(2000, 1), (2300, 1)], 300, seed=1)
+    for hq in (2, 16):
+        cfg, ctx = context(hq, 2, 64)
+        kv = random_arena(cfg, 300, 2)
+        q = torch.randn(rows.T, hq * 64, device="cuda").half()
+        out, alone = torch.empty_like(q), torch.empty_like(q)
+        ctx.kv8_attention(kv, 0, rows.dev, q, out)
+        ctx.kv8_attention(kv, 0, Rows(rows.segs, 300, seed=1).dev, q, alone)
+        assert torch.equal(out, alone) and ctx.status_poll() == 0
+
+
 def test_append_beyond_the_rotary_table_is_reported():
     ctx, kv, rows, q = _small()
     x = torch.randn(rows.T, 12 * 64, device="cuda").half()
