@@ -455,8 +455,8 @@ class KvCache8(KvCache):
         self.arena = None
         if device is not None:
             if arena is not None:
-                if arena.dtype != torch.uint8 or not arena.is_contiguous() or arena.numel() < nbytes or not arena.is_cuda:
-                    raise ValueError("arena: a contiguous uint8 tensor on the GPU that holds n_pages")
+                if arena.dtype != torch.uint8 or arena.dim() != 1 or not arena.is_contiguous() or arena.numel() < nbytes or not arena.is_cuda:
+                    raise ValueError("arena: a contiguous uint8 vector on the GPU that holds n_pages")
                 self.arena = arena[:nbytes]
             else:
                 self.arena = torch.empty(nbytes, dtype=torch.uint8, device=device)

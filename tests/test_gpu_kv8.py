@@ -487,6 +487,20 @@ def test_rows_of_one_step_for_two_models():
         assert torch.equal(out, alone) and ctx.status_poll() == 0
 
 
+def test_arena_of_the_caller():
+    cfg, _ = context(8, 2, 64)
+    n = B.kv8_arena_bytes(cfg, 4)
+    kv = B.KvCache8(cfg, 4, arena=torch.zeros(n + 5, dtype=torch.uint8, device="cuda"))
+    assert kv.codes().shape == (2, 4, 2, 32 * 64) and kv.scales().shape == (2, 4, 2, 2)
+    for bad in (torch.zeros(n - 1, dtype=torch.uint8, device="cuda"), torch.zeros(n, dtype=torch.int8, device="cuda"),
+                torch.zeros(n, dtype=torch.uint8), torch.zeros(2, n, dtype=torch.uint8, device="cuda"),
+                torch.zeros(2 * n, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            B.KvCache8(cfg, 4, arena=bad)
+    with pytest.raises(B.HbError):                     # not 256-byte aligned
+        B.KvCache8(cfg, 4, arena=torch.zeros(n + 16, dtype=torch.uint8, device="cuda")[16:])
+
+
 def test_append_beyond_the_rotary_table_is_reported():
     ctx, kv, rows, q = _small()
     x = torch.randn(rows.T, 12 * 64, device="cuda").half()
