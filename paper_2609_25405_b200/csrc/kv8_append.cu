@@ -6,7 +6,7 @@
 //   block: e = smallest exponent with max |y| <= 448 * 2^e over its new rows (and its old exponent, if the
 //          page already holds rows);  code = e4m3(y * 2^-e)
 //
-// Query warps take 16 heads of one row (8 where latency counts): norm, rotation, store.  The scale of a block
+// Query warps take 8 heads of one row: norm, rotation, store.  The scale of a block
 // of the cache needs all of its new rows at once, so a key / value task is one KV head of one page: the first
 // row of its segment in that page (the leader) and the up to 16 rows that follow it.  DH / 8 lanes
 // share a row, 8 dimensions each: 16-byte loads; the rotary partner (i + rot_dim / 2) sits at the same place of
@@ -18,10 +18,10 @@
 //     whole words of V, so that a page that starts afresh is written in words out of registers.  SHARE tasks
 //     look at the same 16 rows, find such leaders and share what they have to do (looking costs two
 //     dependent loads, so few look).  A page with fewer new rows goes to the query warps of its leader.
-//     4096 rows in 8 chunks, 32 / 8 heads of 128, norms and halves: 46 us = 2.1 TB/s (33 us without norms, in pairs).  No
-//     unit is full (issue slots 45 %): the chain row, segment, page id, old scale and the rows themselves decides, with
-//     the 16 warps per SM that 128 registers allow.  All loads of a query task ahead of its look-up: 51 us (spills);
-//     four of them: 47.
+//     4096 rows in 8 chunks, 32 / 8 heads of 128, norms and halves: 40 us = 2.35 TB/s (30.6 us without norms, in pairs;
+//     26 where the pages begin with the rows).  No unit is full: the chain row, segment, page id, old scale and the
+//     rows themselves decides, with the 16 warps per SM that 128 registers allow.  16 heads a warp 41.6 us, and 21.6
+//     against 18.2 for 64 decode rows and 6 chunks; the rotary tables of both rows of a lane at once (spilled) 50.
 #include <algorithm>
 
 #include "kv8.cuh"
@@ -31,7 +31,7 @@ namespace {
 using namespace hb_kv8;
 
 constexpr int WARPS = 4;
-constexpr int SMALL_ROWS = 3, SHARE = 8;   // see above
+constexpr int SMALL_ROWS = 3, SHARE = 8, HEADS = 8;   // see above
 
 struct AppendParams {
   Rows r;
@@ -185,11 +185,18 @@ __device__ __forceinline__ int new_rows(const RowAt& a, int row) {
 }
 
 // HEADS query heads of a row from head0 on; false for rows of nobody.
-template <int DH, bool HALVES, int HEADS>
+template <int DH, bool HALVES>
 __device__ __forceinline__ bool query_task(const AppendParams& p, int row, int head0, RowAt& a) {
   constexpr int LPR = DH / 8, RPW = 32 / LPR, ITERS = HEADS / RPW;
   const int lane = threadIdx.x & 31, which = lane / LPR, d0 = (lane & (LPR - 1)) * 8;
   const __half* src = p.qkv + row * p.qkv_stride + d0;
+  // all of the warp's loads are in flight together, and while the row's segment and position are looked up
+  uint4 raw[ITERS];
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int head = head0 + it * RPW + which;
+    raw[it] = head < p.Hq ? *reinterpret_cast<const uint4*>(src + head * DH) : make_uint4(0u, 0u, 0u, 0u);
+  }
   bool bad;
   if (!locate(p, row, a, &bad)) {
     if (bad && lane == 0) atomicOr(p.r.status, HB_DEV_APPEND_BAD_INDEX);
@@ -200,28 +207,18 @@ __device__ __forceinline__ bool query_task(const AppendParams& p, int row, int h
   float g[8] = {};
   load_gain(p.q_gain, d0, g);
   __half* dst = p.q_out + row * p.q_stride + d0;
-  // four rows of the head dimension at a time: their loads are in flight together
-#pragma unroll 1
-  for (int it0 = 0; it0 < ITERS && head0 + it0 * RPW < p.Hq; it0 += 4) {
-    uint4 raw[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int head = head0 + (it0 + u) * RPW + which;
-      raw[u] = it0 + u < ITERS && head < p.Hq ? *reinterpret_cast<const uint4*>(src + head * DH) : make_uint4(0u, 0u, 0u, 0u);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (it0 + u >= ITERS) break;
-      const int head = head0 + (it0 + u) * RPW + which;
-      float x[8];
-      unpack8(raw[u], x);
-      norm_rotate<DH, HALVES>(p, g, p.q_gain != nullptr, t, x);
-      if (head < p.Hq) {
-        uint4 o;
-        o.x = pack_half2_sat2(x[0], x[1]); o.y = pack_half2_sat2(x[2], x[3]);
-        o.z = pack_half2_sat2(x[4], x[5]); o.w = pack_half2_sat2(x[6], x[7]);
-        *reinterpret_cast<uint4*>(dst + head * DH) = o;
-      }
+  for (int it = 0; it < ITERS; ++it) {
+    if (head0 + it * RPW >= p.Hq) break;
+    const int head = head0 + it * RPW + which;
+    float x[8];
+    unpack8(raw[it], x);
+    norm_rotate<DH, HALVES>(p, g, p.q_gain != nullptr, t, x);
+    if (head < p.Hq) {
+      uint4 o;
+      o.x = pack_half2_sat2(x[0], x[1]); o.y = pack_half2_sat2(x[2], x[3]);
+      o.z = pack_half2_sat2(x[4], x[5]); o.w = pack_half2_sat2(x[6], x[7]);
+      *reinterpret_cast<uint4*>(dst + head * DH) = o;
     }
   }
   return true;
@@ -363,17 +360,17 @@ __device__ __forceinline__ int old_exponent(const uint8_t* block, int slot0, int
   return slot0 == 0 ? E_MIN : max(E_MIN, min(E_MAX, exponent_of(reinterpret_cast<const float*>(block + Block<DH>::HDR)[is_v])));
 }
 
+// (One row after the other: the tables of both would not leave enough registers for the queries.)
 template <int DH, bool HALVES, int N>
 __device__ __forceinline__ void key_rows(const AppendParams& p, const int (&pos)[N], int d0, const uint4 (&raw)[N], float (&x)[N][8]) {
-  Turn t[N];
-#pragma unroll
-  for (int it = 0; it < N; ++it) load_turn<DH, HALVES>(p, pos[it], d0, t[it]);
   float g[8] = {};
   load_gain(p.k_gain, d0, g);
 #pragma unroll
   for (int it = 0; it < N; ++it) {
+    Turn t;
+    load_turn<DH, HALVES>(p, pos[it], d0, t);
     unpack8(raw[it], x[it]);
-    norm_rotate<DH, HALVES>(p, g, p.k_gain != nullptr, t[it], x[it]);
+    norm_rotate<DH, HALVES>(p, g, p.k_gain != nullptr, t, x[it]);
   }
 }
 
@@ -421,9 +418,10 @@ __device__ __forceinline__ void page_task(const AppendParams& p, int row, const 
 #pragma unroll
   for (int it = 0; it < S::ITERS; ++it) {
     at[it] = sl.have[it] ? pos - sl.slot0 + sl.at(it) : pos;
-    unpack8(raw_v[it], xv[it]);
   }
   key_rows<DH, HALVES>(p, at, sl.d0, raw_k, xk);
+#pragma unroll
+  for (int it = 0; it < S::ITERS; ++it) unpack8(raw_v[it], xv[it]);
   float2 m = make_float2(amax_of(xk), amax_of(xv));
   __syncthreads();   // the maxima of the block's last task have been read
   if ((threadIdx.x & 31) == 0) warp_max[sl.warp] = m;
@@ -445,7 +443,7 @@ kv8_append_small_kernel(const AppendParams p, const int q_per_row, const int tas
   if (row >= p.r.n_rows) return;
   RowAt a;
   if (task < q_per_row) {
-    query_task<DH, HALVES, 8>(p, row, task * 8, a);
+    query_task<DH, HALVES>(p, row, task * HEADS, a);
     return;
   }
   bool bad;
@@ -468,7 +466,7 @@ kv8_append_kernel(const AppendParams p, const int q_per_row, const int q_tasks, 
       const int64_t at = static_cast<int64_t>(task) * WARPS + warp;
       const int row = static_cast<int>(at / q_per_row), share = static_cast<int>(at % q_per_row);
       RowAt a;
-      if (row >= p.r.n_rows || !query_task<DH, HALVES, 16>(p, row, share * 16, a)) continue;
+      if (row >= p.r.n_rows || !query_task<DH, HALVES>(p, row, share * HEADS, a)) continue;
       if (!leads(a, row) || new_rows(a, row) > SMALL_ROWS) continue;
       for (int kv = share; kv < n_kv; kv += q_per_row) {
         if (kv < p.r.Hkv) small_task<DH, HALVES, false>(p, row, a, kv);
@@ -500,12 +498,12 @@ template <int DH, bool HALVES>
 int launch(const AppendParams& p, int num_sms, cudaStream_t s, bool pdl) {
   const long long rows = p.r.n_rows;
   if (p.r.max_q_len <= SMALL_ROWS) {
-    const int q_per_row = (p.Hq + 7) / 8, tasks = q_per_row + 2 * p.r.Hkv;
+    const int q_per_row = (p.Hq + HEADS - 1) / HEADS, tasks = q_per_row + 2 * p.r.Hkv;
     const long long blocks = (rows * tasks + WARPS - 1) / WARPS;
     if (blocks > 0x7fffffffll) return HB_ERR_TOO_LARGE;
     return hb_launch_kernel(kv8_append_small_kernel<DH, HALVES>, static_cast<unsigned>(blocks), WARPS * 32, 0, s, pdl, p, q_per_row, tasks);
   }
-  const int q_per_row = (p.Hq + 15) / 16;
+  const int q_per_row = (p.Hq + HEADS - 1) / HEADS;
   const long long q_tasks = (rows * q_per_row + WARPS - 1) / WARPS, n_tasks = q_tasks + (rows + 15) / 16 * SHARE;
   if (n_tasks > 0x7fffffffll) return HB_ERR_TOO_LARGE;
   return hb_launch_kernel(kv8_append_kernel<DH, HALVES>, static_cast<unsigned>(std::min<long long>(n_tasks, 4ll * num_sms)), WARPS * 32, 0, s, pdl,
