@@ -575,11 +575,11 @@ constexpr int JOIN_WARPS = 4;
 template <int DH>
 __global__ void __launch_bounds__(JOIN_WARPS * 32)
 kv8_join_kernel(const AttnParams p) {
+  grid_dep_wait();   // (the segments as much as the records)
   grid_dep_launch();
   const int seg = blockIdx.x / p.r.Hkv, head = blockIdx.x % p.r.Hkv, lane = threadIdx.x & 31;
   Seg g;
-  const int ns = load_seg(p.r, seg, g) ? splits_of(p, g) : 0;   // (the rows are inputs: they are there before the records)
-  grid_dep_wait();   // every block, so that this grid does not end before the ones in front of it
+  const int ns = load_seg(p.r, seg, g) ? splits_of(p, g) : 0;
   if (ns <= 1) return;
   constexpr int V = DH / 32;   // dimensions per lane
   for (int c = threadIdx.x >> 5; c < g.q_len * p.r.G; c += JOIN_WARPS) {

@@ -127,8 +127,6 @@ __device__ __forceinline__ void tc_item(const Rows& r, const int* prefix, int id
 template <int DH>
 __global__ void __launch_bounds__(THREADS, 1)
 kv8_chunk_kernel(const AttnParams p) {
-  // Launched behind the decode kernel, whose blocks have all waited for what was before them; it reads nothing of
-  // that kernel's, so it takes an SM as soon as the decode blocks there are done, and waits for the rest at its end.
   using C = Cfg<DH>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -144,8 +142,8 @@ kv8_chunk_kernel(const AttnParams p) {
   int* warp_sums = reinterpret_cast<int*>(smem + C::MISC_OFF + 64);
   int* prefix = reinterpret_cast<int*>(smem + C::FIXED);
   if (base & 1023u) {   // the swizzled tiles need it; the same in every thread
-    if (tid == 0) atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
     grid_dep_wait();
+    if (tid == 0) atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
     return;
   }
   if (tid == 0) {
@@ -166,6 +164,10 @@ kv8_chunk_kernel(const AttnParams p) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  // A block may take its SM, its barriers and its tensor memory while the decode kernel drains; what it reads (the
+  // segments, the queries, the pages appended by the launch before) is only sure to be there behind the wait.  That the
+  // decode blocks have waited for it themselves orders the execution, and makes nothing visible here.
+  grid_dep_wait();
   const int total = build_prefix<THREADS>(p.r, prefix, warp_sums, [&](const Seg& g) { return tc_blocks(p.r, g) * p.r.Hkv; }, false);
   const uint16_t* order = nullptr;
   const int n_blocks = total / p.r.Hkv;
@@ -523,7 +525,6 @@ kv8_chunk_kernel(const AttnParams p) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
-  grid_dep_wait();
 }
 
 }  // namespace hb_kv8_tc

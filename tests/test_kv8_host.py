@@ -1,5 +1,7 @@
 """The 8-bit KV cache on the host: sizes, refusals, page bookkeeping, rotary tables, the oracle's pins.  No GPU."""
 import ctypes as C
+import os
+import re
 
 import numpy as np
 import pytest
@@ -149,3 +151,44 @@ def test_oracle_attention_is_softmax_attention():
     to = lambda a, rep: torch.from_numpy(a).transpose(0, 1).repeat_interleave(rep, 0)  # noqa: E731
     ref = torch.nn.functional.scaled_dot_product_attention(to(q, 1), to(k, 2), to(v, 2), attn_mask=mask, scale=0.125)
     assert np.max(np.abs(out - ref.transpose(0, 1).numpy())) < 1e-13
+
+
+def _kernels():
+    """(name, body) of every kernel of the library's sources."""
+    csrc = os.path.join(os.path.dirname(B.__file__), "csrc")
+    for f in sorted(os.listdir(csrc)):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, f)).read())
+        for m in re.finditer(r"__global__ void (?:__launch_bounds__\((?:[^()]|\([^()]*\))*\)|__maxnreg__\(\d+\))?\s*(\w+)\(", text):
+            at = start = text.index("{", m.end())
+            depth = 0
+            while True:
+                depth += {"{": 1, "}": -1}.get(text[at], 0)
+                at += 1
+                if depth == 0:
+                    break
+            yield m.group(1), text[start + 1:at - 1]
+
+
+def _before_wait(body):
+    """The part of a kernel before its own wait for the launch in front of it (one that every path takes), or None."""
+    for m in re.finditer(r"grid_dep_wait\(\)", body):
+        head = body[:m.start()]
+        if head.count("{") == head.count("}"):
+            return head
+    return None
+
+
+def test_kernels_read_nothing_before_they_wait():
+    """A kernel that may be resident while the launch before it drains sees what came before only behind griddepcontrol.wait,
+    whatever that launch has waited for itself: no segment, row, page id or query is read ahead of it."""
+    reads = re.compile(r"__ldg|load_seg|build_prefix|find_item|tc_item|locate\(|load_ids|bulk_load")
+    heads = {name: _before_wait(body) for name, body in _kernels() if "grid_dep_" in body}
+    assert {"kv8_append_small_kernel", "kv8_append_kernel", "kv8_attend_kernel", "kv8_chunk_kernel", "kv8_join_kernel",
+            "attn_varlen_kernel", "norm_kernel"} <= set(heads)
+    for name, head in heads.items():
+        assert head is not None, name
+        assert not reads.search(head), (name, reads.search(head).group())
+    for f in ("kv8_append.cu", "kv8_attention.cu", "attention.cu", "elementwise.cu"):   # every launch that may overlap names such a kernel
+        text = open(os.path.join(os.path.dirname(B.__file__), "csrc", f)).read()
+        for m in re.finditer(r"hb_launch_kernel\((\w+)", text):
+            assert m.group(1) in heads or m.group(1) in ("kern", "tc"), m.group(1)
