@@ -394,16 +394,18 @@ __device__ __forceinline__ int warp_pages(const Item& it) {
   const int warp = threadIdx.x >> 5, n = (it.key1 + PAGE - 1) / PAGE - it.key0 / PAGE;
   return n > warp ? (n - warp + DEC_WARPS - 1) / DEC_WARPS : 0;
 }
-// Page ids of the warp's pages [batch, batch + 32) of an item, one per lane (-2: none).
+// Page ids of the warp's pages [batch, batch + 32) of an item, one per lane (lanes behind the last page: 0).
 __device__ __forceinline__ int load_ids(const AttnParams& p, const Item& it, int batch) {
   const int i = batch + (threadIdx.x & 31);
-  return i < warp_pages(it) ? __ldg(p.r.page_ids + it.g.pt_start + it.key0 / PAGE + (threadIdx.x >> 5) + i * DEC_WARPS) : -2;
+  return i < warp_pages(it) ? __ldg(p.r.page_ids + it.g.pt_start + it.key0 / PAGE + (threadIdx.x >> 5) + i * DEC_WARPS) : 0;
 }
-// Checks a batch of ids and asks for its first pages.  False (and a report) if one is no page: nothing is asked for.
+// Checks a batch of n ids (or 32, if there are more) and asks for its first pages.  False (and a report) if one is no
+// page: nothing is asked for.  Which lanes have an id follows from n: no value of an id stands for "none".
 template <int DH>
 __device__ __forceinline__ bool start_batch(const AttnParams& p, const Item& it, int id, int n, Ring& ring) {
-  if (__any_sync(0xffffffffu, id != -2 && (id < 0 || id >= p.r.n_pages))) {
-    if ((threadIdx.x & 31) == 0) atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
+  const int lane = threadIdx.x & 31;
+  if (__any_sync(0xffffffffu, lane < n && (id < 0 || id >= p.r.n_pages))) {
+    if (lane == 0) atomicOr(p.r.status, HB_DEV_ATTN_BAD_INDEX);
     return false;
   }
   for (int i = 0; i < min(n, STAGES); ++i) request<DH>(p, ring, __shfl_sync(0xffffffffu, id, i), it.head);
@@ -532,7 +534,7 @@ kv8_attend_kernel(const AttnParams p) {
   mbar_init_fence();
   const int total = build_prefix<DEC_THREADS>(p.r, prefix, warp_sums, [&](const Seg& g) { return splits_of(p, g) * p.r.Hkv; }, true);   // its barriers publish the initialisation
   Item it;
-  int id = -2;
+  int id = 0;
   bool ok = true;
   if (static_cast<int>(blockIdx.x) < total) {
     find_item(p, prefix, blockIdx.x, it);
@@ -543,7 +545,7 @@ kv8_attend_kernel(const AttnParams p) {
     // the next item and its page ids are looked up before this one's pages are computed
     const int next = idx + gridDim.x;
     Item nit = it;
-    int nid = -2;
+    int nid = 0;
     bool nok = true;
     if (next < total) {
       find_item(p, prefix, next, nit);

@@ -449,6 +449,42 @@ def test_bad_page_ids_and_segments_are_reported_and_skipped():
     assert ctx.status_poll() == 4
 
 
+@pytest.mark.parametrize("bad", [-1, -2, -3, -2 ** 31, 400, 2 ** 31 - 1])
+def test_no_page_id_outside_the_arena_is_followed(bad):
+    """Any id outside the arena, at the first, a middle and the last page of a decode row (one split and several, any of the
+    four warps, behind a warp's first 32 pages), of a row with two column tiles and of a chunk, and at the page that an
+    append writes: reported, the segment's rows left alone, the other segments right."""
+    cfg, ctx = context(16, 2, 64)
+    kv = random_arena(cfg, 400, 3)
+    segs = [(200, 1), (3000, 1), (90, 2), (100, 20), (17, 1), (480, 1), (30, 1)]
+    rows = Rows(segs, 400, seed=3)
+    q = torch.randn(rows.T, 16 * 64, device="cuda").half()
+    good = torch.empty_like(q)
+    ctx.kv8_attention(kv, 0, rows.dev, q, good)
+    assert ctx.status_poll() == 0
+    for i, (p, n) in enumerate(segs[:6]):
+        first, count = rows.table[i, 4], (p + n + 15) // 16
+        for at in sorted({0, 1, 2, 3, min(40, count - 1), count // 2, count - 1} & set(range(count))):
+            ids = rows.dev.page_ids.clone()
+            ids[int(first) + at] = bad
+            out = torch.full_like(q, -3.0)
+            ctx.kv8_attention(kv, 0, B.SegRows(rows.dev.segs, ids, rows.dev.row_seg, 20, 3001), q, out)
+            assert ctx.status_poll() == 2, (i, at)
+            gone = torch.zeros(rows.T, dtype=torch.bool, device="cuda")
+            gone[rows.start[i]:rows.start[i] + n] = True
+            assert torch.all(out[gone] == -3.0) and torch.equal(out[~gone], good[~gone]), (i, at)
+    arena = kv.arena.clone()
+    x = torch.randn(rows.T, 20 * 64, device="cuda").half()
+    for i, (p, n) in enumerate(segs):
+        ids = rows.dev.page_ids.clone()
+        ids[int(rows.table[i, 4]) + p // 16] = bad
+        before = kv.codes()[0, rows.pages[i][p // 16]].view(torch.uint8).clone()
+        ctx.kv8_append(kv, 0, B.SegRows(rows.dev.segs, ids, rows.dev.row_seg, 20, 3001), x, torch.empty_like(q))
+        assert ctx.status_poll() == 4, i
+        assert torch.equal(kv.codes()[0, rows.pages[i][p // 16]].view(torch.uint8), before), i
+        kv.arena.copy_(arena)
+
+
 def test_many_chunks_with_bad_pages():
     """Short chunks, two out of three of them with a page id outside the arena, several of those in a row for every
     block: none of their rows is written, all others are right."""
