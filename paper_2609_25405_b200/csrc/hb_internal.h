@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <mutex>
 #include <vector>
 
 #include "../../include/hb.h"
@@ -148,19 +149,26 @@ int hb_tmap_2d_f16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t c
 
 // Dynamic shared memory above 48 KiB has to be enabled per kernel ON EVERY DEVICE the kernel runs
 // on.  One of these per kernel instantiation remembers, per device, the largest size enabled so
-// far; hb_ensure_dyn_smem raises it on the current device when a launch needs more.
+// far; hb_ensure_dyn_smem raises it on the current device when a launch needs more.  Threads that launch the
+// same kernel with different sizes take turns there: a smaller size set behind a larger one would take back what
+// `bytes` says is enabled.
 constexpr int HB_MAX_DEVICES = 64;
 struct DynSmemState {
   std::atomic<int> bytes[HB_MAX_DEVICES];
+  std::mutex raise;
 };
 inline int hb_ensure_dyn_smem(const void* kern, DynSmemState& st, int bytes) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= HB_MAX_DEVICES) return HB_ERR_CUDA;
   if (st.bytes[dev].load(std::memory_order_acquire) >= bytes) return HB_OK;
-  // two threads may both get here: the attribute call is idempotent
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return HB_ERR_CUDA;
-  int seen = st.bytes[dev].load(std::memory_order_relaxed);
-  while (seen < bytes && !st.bytes[dev].compare_exchange_weak(seen, bytes, std::memory_order_release)) {}
+  try {
+    const std::lock_guard<std::mutex> turn(st.raise);
+    if (st.bytes[dev].load(std::memory_order_relaxed) >= bytes) return HB_OK;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return HB_ERR_CUDA;
+    st.bytes[dev].store(bytes, std::memory_order_release);
+  } catch (...) {   // (a mutex may throw; nothing may leave a C entry point)
+    return HB_ERR_CUDA;
+  }
   return HB_OK;
 }
 // GEMM variants: 128 / 256 = one CTA per 128 x BN tile; HB_GEMM_PAIR256 = a CTA pair per 256 x 256 tile.
