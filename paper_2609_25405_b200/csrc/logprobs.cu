@@ -73,9 +73,9 @@ __device__ __forceinline__ Rec join(Rec a, Rec b) {
   return Rec{a.m, fmaf(f, w, a.T), fmaf(f, fmaf(d, w, b.S), a.S)};
 }
 
-// Orderable bits of a logit; NaN below -inf.
+// Orderable bits of a logit; NaN below -inf, both zeros alike (-0 + 0 is +0).
 __device__ __forceinline__ uint32_t order(float x) {
-  const uint32_t u = __float_as_uint(x);
+  const uint32_t u = __float_as_uint(x + 0.0f);
   return x != x ? 0u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 __device__ __forceinline__ uint64_t make_key(float x, int idx) { return (static_cast<uint64_t>(order(x)) << 32) | static_cast<uint32_t>(~idx); }

@@ -92,6 +92,40 @@ def test_arrangements_that_are_hard_on_the_selection(order, vocab):
         _check(x, k)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("n,vocab", [(1, 40), (5, 20000), (1, 128256), (40, 128256), (500, 33001)])
+def test_zeros_of_either_sign_are_equal(n, vocab, dtype):
+    """-0 and +0 are equal logits: the lower token comes first, inside a slice, across slices and across the blocks that share a
+    row; as the best logits, between larger and smaller ones, and in rows of nothing else."""
+    r = np.random.default_rng(vocab + n)
+    x = -np.abs(r.standard_normal((n, vocab))) - 0.5
+    for i in range(n):
+        at = r.choice(vocab, min(vocab // 2, 30), replace=False)
+        x[i, at] = np.where(r.integers(0, 2, len(at)) == 1, 0.0, -0.0)
+        if i % 3 == 1:
+            x[i, at[:3]] = 2.0
+    x[0, np.argmax(x[0] == 0.0)] = -0.0                    # the first zero is a negative one
+    if n > 2:
+        x[2] = np.where(np.arange(vocab) % 2 == 0, -0.0, 0.0)
+    t = torch.from_numpy(x).to(dtype).cuda()
+    for k in (1, 7, min(32, vocab)):
+        _check(t, k)
+
+
+def test_zeros_of_either_sign_and_argmax():
+    """The first alternative is hb_argmax's token in rows whose largest logits are zeros of both signs."""
+    from paper_2609_25405_b200 import synth
+    ctx = B.Context(B.model_cfg(synth.ModelShape("v", 1, 64, 1, 1, 64, 64, 32000), 16), 1, 1, 1)
+    x = -torch.rand(4, 32000, device="cuda") - 0.1
+    for i, (neg, pos) in enumerate(((5, 9), (9, 5), (100, 31000), (31000, 100))):
+        x[i, neg], x[i, pos] = -0.0, 0.0
+    tok, ids, top = torch.empty(4, dtype=torch.int32, device="cuda"), torch.empty(4, 2, dtype=torch.int32, device="cuda"), torch.empty(4, 2, device="cuda")
+    ctx.argmax(x, 4, tok)
+    ctx.logprobs(x, None, None, None, ids, top)
+    assert torch.equal(tok, ids[:, 0]) and tok.tolist() == [5, 5, 100, 100] and torch.equal(top[:, 0], top[:, 1])
+    ctx.close()
+
+
 def test_nearly_certain_rows_keep_their_entropy():
     """One logit 5 .. 60 above the rest: the entropy and -log p of the best are tiny and right to 2^-17 relative."""
     gap = torch.arange(5.0, 61.0, 5.0, device="cuda")
