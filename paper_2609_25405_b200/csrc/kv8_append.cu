@@ -289,10 +289,10 @@ __device__ __forceinline__ void store_part(const Slots<DH, SMALL>& sl, uint8_t* 
     uint8_t* dst = part + (d0 >> 6) * 1024 + (d0 & 63);
 #pragma unroll
     for (int it = 0; it < S::ITERS; ++it) {
-      if (sl.have[it] || (fresh && !SMALL))
-        *reinterpret_cast<uint2*>(dst + sl.at(it) * 64) =
-            make_uint2(floats_to_e4m3x4(x[it][0] * inv, x[it][1] * inv, x[it][2] * inv, x[it][3] * inv),
-                       floats_to_e4m3x4(x[it][4] * inv, x[it][5] * inv, x[it][6] * inv, x[it][7] * inv));
+      uint2 codes = make_uint2(floats_to_e4m3x4(x[it][0] * inv, x[it][1] * inv, x[it][2] * inv, x[it][3] * inv),
+                               floats_to_e4m3x4(x[it][4] * inv, x[it][5] * inv, x[it][6] * inv, x[it][7] * inv));
+      if (!sl.have[it]) codes = make_uint2(0u, 0u);   // (norm and rotation may have made NaN of the zeros of no row)
+      if (sl.have[it] || (fresh && !SMALL)) *reinterpret_cast<uint2*>(dst + sl.at(it) * 64) = codes;
     }
   } else if (SMALL || !fresh) {
 #pragma unroll

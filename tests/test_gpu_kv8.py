@@ -157,6 +157,35 @@ def test_append_of_zeros_extremes_and_nan():
         assert c.exps[which][pg[4], 0] == -32 and np.all(c.codes[which][pg[4], 0, :4] == 256.0)
 
 
+@pytest.mark.parametrize("dh,halves", [(64, False), (64, True), (128, False), (128, True)])
+@pytest.mark.parametrize("odd", ["no epsilon", "gain", "table"])
+def test_unused_slots_of_a_fresh_block_become_zero(dh, halves, odd):
+    """Whatever the norm and the rotation make of nothing: an epsilon of zero (0 / 0), a gain or a rotary factor that is not finite."""
+    cfg, ctx = context(4, 2, dh)
+    kv = B.KvCache8(cfg, 12, fill=0xFF)
+    rows = Rows([(0, 1), (0, 3), (0, 4), (16, 11), (5, 20), (0, 16)], 12, seed=4)
+    x = torch.randn(rows.T, 8 * dh, device="cuda").half()
+    gain = torch.ones(dh, device="cuda").bfloat16()
+    cos, sin = (torch.from_numpy(t).cuda() for t in B.rope_table(32, dh, 1e4))
+    if odd == "gain":
+        gain[3] = float("inf")
+    if odd == "table":
+        cos[:, 1] = float("nan")
+    out = torch.empty(rows.T, 4 * dh, dtype=torch.float16, device="cuda")
+    ctx.kv8_append(kv, 0, rows.dev, x, out, rope=B.Rope(cos, sin, B.ROPE_HALVES if halves else B.ROPE_PAIRS), q_norm=gain, k_norm=gain,
+                   norm_eps=0.0 if odd == "no epsilon" else EPS)
+    assert ctx.status_poll() == 0
+    c = oracle_layer(kv, 0)
+    for (p, n), pages in zip(rows.segs, rows.pages):
+        for b in range(p // 16, (p + n + 15) // 16):
+            lo, hi = max(p - b * 16, 0), min(p + n - b * 16, 16)
+            for which in range(2):
+                if lo == 0:
+                    assert np.all(c.codes[which][pages[b]][:, hi:] == 0.0), (which, p, n, b)
+                if odd == "no epsilon":
+                    assert np.all(np.isfinite(c.codes[which][pages[b]][:, lo:hi]))
+
+
 def test_append_in_place_of_the_qkv_rows():
     """q_out may be the q part of qkv."""
     cfg, ctx = context(8, 2, 128)
