@@ -44,6 +44,9 @@ constexpr int RAW = 3, CV = 3;           // stages of the ring of codes, of conv
 constexpr int BAD = 8;
 static_assert(BAD > RAW + CV + 1 && (BAD & (BAD - 1)) == 0, "slots of bad items");
 constexpr uint64_t WAIT_NS = 1000000000ull;
+// Least factor of the scores (the smallest normal float): zero times the -inf of a key that a row must not see would be
+// NaN.  Scores are below 2^32, so that neither it nor anything smaller leaves anything of them.
+constexpr float FACTOR_MIN = 1.1754944e-38f;
 
 template <int DH>
 struct Cfg {
@@ -303,7 +306,7 @@ kv8_chunk_kernel(const AttnParams p) {
         float2 sc = make_float2(1.0f, 0.0f);
         if (left > 0) {
           asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(sc.x), "=f"(sc.y) : "r"(src + Block<DH>::HDR));
-          sc.x *= p.scale_log2;
+          sc.x = fmaxf(sc.x * p.scale_log2, FACTOR_MIN);
           sc.y = static_cast<float>(exponent_of(sc.y));
         }
         if (lane == 0) *reinterpret_cast<float2*>(smem + C::SC_OFF + (cs * PAGES + pg) * 8) = sc;

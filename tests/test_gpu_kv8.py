@@ -308,6 +308,17 @@ def test_sharp_and_flat_softmax():
         assert np.all(err <= attend_bound(mass, p + n, np.abs(V).max()) + mass * s_max * 2.0 ** -20 + np.abs(V).max() * s_max * 2.0 ** -22)
 
 
+@pytest.mark.parametrize("scale", [1e-38, 1e-36, 2.0 ** -90])
+def test_scales_that_leave_nothing_of_the_scores(scale):
+    """The factor of the scores times a block's scale may be too small for fp32: every key counts the same, and none that a row
+    must not see, in decode rows, splits and chunks."""
+    cfg, ctx = context(8, 2, 128)
+    kv = random_arena(cfg, 150, 4)
+    kv.scales()[..., 0] = 2.0 ** -32
+    rows = Rows([(700, 1), (3, 40), (511, 1), (90, 5), (64, 130), (0, 2)], 150)
+    _check_attend(ctx, kv, 0, rows, 8, 2, 128, 5, scale=scale)
+
+
 def test_stale_bytes_behind_the_last_key():
     """NaN codes in the unused slots of a request's last page, and in pages of nobody, do not reach any row."""
     cfg, ctx = context(8, 2, 128)
