@@ -47,6 +47,10 @@ constexpr uint64_t WAIT_NS = 1000000000ull;
 // Least factor of the scores (the smallest normal float): zero times the -inf of a key that a row must not see would be
 // NaN.  Scores are below 2^32, so that neither it nor anything smaller leaves anything of them.
 constexpr float FACTOR_MIN = 1.1754944e-38f;
+// A weight's exponent is formed in one step, score * factor + (e - m), whose product is not rounded, while m came from a
+// rounded one, so that it may end above its bound by 2^-23 of m.  Up to 2^20 that is no more than the score's own rounding;
+// further out the weights could leave fp16 (from 2^24 on), and the scores are rounded first, as in the maximum.
+constexpr float FAR = 1048576.0f;
 
 template <int DH>
 struct Cfg {
@@ -395,6 +399,7 @@ kv8_chunk_kernel(const AttnParams p) {
         if (lane == 0) mbar_arrive(q_ready0 + 8u * x);
       }
       float m = -INFINITY, l = 0.0f;
+      bool far = false;   // a row of the warp has its maximum beyond FAR
       for (int j = 0; j < n_tiles; ++j) {
         if (!wait(s_full0 + 8u * x, n_s & 1u)) break;
         ++n_s;
@@ -437,7 +442,7 @@ kv8_chunk_kernel(const AttnParams p) {
         }
         // P stays below 2^14: its reference lies 6 below the maximum it was taken from
         const bool grow = mx > m + 14.0f || (m == -INFINITY && mx > -INFINITY);
-        if (__any_sync(0xffffffffu, grow)) {
+        if (__any_sync(0xffffffffu, grow || far)) {
           const float m_new = grow ? mx - 6.0f : m;
           const float f = grow ? ex2_approx(m - m_new) : 1.0f;   // -inf -> 0
           if (j > 0) {   // (S of this tile was issued behind the last P V: O is complete)
@@ -453,8 +458,21 @@ kv8_chunk_kernel(const AttnParams p) {
           }
           l *= f;
           m = m_new;
+          far = __any_sync(0xffffffffu, m > FAR || (m < -FAR && m > -INFINITY));
+          if (far) {   // exponents out of rounded scores (e, taken off here, is added below: a rounding of 2^-16 at most)
+            const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+            for (int g = 0; g < PAGES; ++g) {
+#pragma unroll
+              for (int i = 0; i < PAGE; ++i) {
+                uint32_t& s = sr[g >> 1][(g & 1) * PAGE + i];
+                s = __float_as_uint(fmaf(__uint_as_float(s), sc[g].x, sc[g].y) - ref - sc[g].y);
+              }
+              sc[g].x = 1.0f;
+            }
+          }
         }
-        const float neg_m = m == -INFINITY ? 0.0f : -m;
+        const float neg_m = far || m == -INFINITY ? 0.0f : -m;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {   // two pages, then the other two: the first half of P V starts early
           uint32_t pk[16];

@@ -319,6 +319,34 @@ def test_scales_that_leave_nothing_of_the_scores(scale):
     _check_attend(ctx, kv, 0, rows, 8, 2, 128, 5, scale=scale)
 
 
+@pytest.mark.parametrize("scale", [0.0, 1.0, 2.0 ** 30, 2.0 ** 60])
+def test_scores_beyond_a_million(scale):
+    """Queries of 60000, keys of one dimension each with values on the codes of e4m3: scores of 2^20 to 2^90, whose largest takes all;
+    neighbouring values differ by 2^-4 of themselves at least, and equal ones are equal in fp32 too (V's scales are one).  Positive
+    and negative scores, decode rows, splits and chunks."""
+    cfg, ctx = context(8, 2, 64)
+    kv = random_arena(cfg, 150, 4, 0, 0)
+    t, d = np.arange(16)[:, None], np.arange(64)[None, :]
+    a = layer_bytes(kv, 0).copy()
+    r = np.random.default_rng(3)
+    a[..., :16 * 64] = 0
+    a[..., O.k_byte(np.arange(16), 0)] = r.integers(0x40, 0x7F, (150, 2, 16)) | (np.arange(2)[None, :, None] << 7)   # head 1: negative keys
+    kv.arena[:a.size] = torch.from_numpy(a.reshape(-1)).cuda()
+    kv.scales()[..., 0] = 2.0 ** 8
+    rows = Rows([(700, 1), (3, 40), (511, 1), (90, 5), (64, 130), (0, 2), (20, 1)], 150)
+    q = torch.zeros(rows.T, 8, 64, dtype=torch.float16, device="cuda")
+    q[:, :, 0] = 60000.0
+    out = torch.empty(rows.T, 512, dtype=torch.float16, device="cuda")
+    ctx.kv8_attention(kv, 0, rows.dev, q.view(rows.T, 512), out, scale=scale)
+    assert ctx.status_poll() == 0
+    cache, got, qn = oracle_layer(kv, 0), out.cpu().numpy().astype(np.float64), q.cpu().numpy().astype(np.float64)
+    for (p, n), at, pages in zip(rows.segs, rows.start, rows.pages):
+        K, V = (cache.rows(w, pages, p + n) for w in range(2))
+        ref, mass = O.attend(qn[at:at + n], K, V, p, scale or 0.125)
+        err = np.abs(got[at:at + n].reshape(n, 8, 64) - ref)
+        assert np.all(err <= attend_bound(mass, p + n, np.abs(V).max())), ((p, n), np.max(err))
+
+
 def test_stale_bytes_behind_the_last_key():
     """NaN codes in the unused slots of a request's last page, and in pages of nobody, do not reach any row."""
     cfg, ctx = context(8, 2, 128)
