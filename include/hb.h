@@ -549,7 +549,7 @@ HB_API int hb_kv8_append(hb_ctx* ctx, hb_kv* kv, int32_t layer, const hb_rows* r
  * v included: append first): row j of a segment sees positions 0 .. pos_start + j.
  *   q    fp16 [n_rows, q_stride], out fp16 [n_rows, out_stride]: n_heads heads of head_dim; 16-byte
  *        aligned, strides multiples of 8; out may not overlap q
- *   scale  factor of the scores (0 = 1 / sqrt(head_dim))
+ *   scale  factor of the scores, up to 2^60 (0 = 1 / sqrt(head_dim)): with it the scores of finite q and k are finite
  *   workspace  device, 256-byte aligned, hb_kv8_attention_workspace bytes for these rows; needs no
  *        initialisation and belongs to the call until it has run: calls that may run at the same
  *        time need a workspace each

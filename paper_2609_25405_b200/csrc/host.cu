@@ -635,7 +635,7 @@ int hb_kv8_attention(hb_ctx* c, hb_kv* kv, int32_t layer, const hb_rows* rows, c
   const int64_t n_q = static_cast<int64_t>(c->cfg.n_heads) * c->cfg.head_dim;
   if (q_stride < n_q || q_stride % 8 || out_stride < n_q || out_stride % 8) return HB_ERR_BAD_ARG;
   if (misaligned(q, 16) || misaligned(out, 16)) return HB_ERR_BAD_ARG;
-  if (!(scale >= 0.0f) || !(scale <= 3.0e38f)) return HB_ERR_BAD_ARG;
+  if (!(scale >= 0.0f) || !(scale <= 1152921504606846976.0f)) return HB_ERR_BAD_ARG;   // (2^60: no score overflows)
   const size_t need = hb_kv8_attention_scratch(c->cfg, r.n_rows, r.n_segs, r.max_keys, hb_kv8_min_split_keys());
   if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 256))) return HB_ERR_BAD_ARG;
   if (r.n_rows == 0 || r.n_segs == 0 || r.max_q_len == 0) return HB_OK;

@@ -347,6 +347,24 @@ def test_scores_beyond_a_million(scale):
         assert np.all(err <= attend_bound(mass, p + n, np.abs(V).max())), ((p, n), np.max(err))
 
 
+def test_scales_up_to_their_limit():
+    """2^60 keeps every score finite (65504 * 448 * 2^24 * 128 * 2^60 log2(e) < 2^117): queries of zero still give the mean, and
+    anything above is refused."""
+    cfg, ctx = context(8, 2, 64)
+    kv = random_arena(cfg, 100, 4)
+    kv.scales()[..., 0] = 2.0 ** 24
+    rows = Rows([(700, 1), (3, 40), (20, 1)], 100)
+    _check_attend(ctx, kv, 0, rows, 8, 2, 64, 5, scale=2.0 ** 60, q_scale=0.0)
+    q = torch.full((rows.T, 512), 65504.0, dtype=torch.float16, device="cuda")
+    out = torch.empty_like(q)
+    ctx.kv8_attention(kv, 0, rows.dev, q, out, scale=2.0 ** 60)
+    assert bool(torch.isfinite(out).all()) and ctx.status_poll() == 0
+    for scale in (2.0 ** 60 * 1.001, 1e30, 3e38):
+        with pytest.raises(B.HbError) as e:
+            ctx.kv8_attention(kv, 0, rows.dev, q, out, scale=scale)
+        assert e.value.code == -1
+
+
 def test_stale_bytes_behind_the_last_key():
     """NaN codes in the unused slots of a request's last page, and in pages of nobody, do not reach any row."""
     cfg, ctx = context(8, 2, 128)
