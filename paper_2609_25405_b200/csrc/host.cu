@@ -638,7 +638,7 @@ int hb_kv8_attention(hb_ctx* c, hb_kv* kv, int32_t layer, const hb_rows* rows, c
   if (!(scale >= 0.0f) || !(scale <= 1152921504606846976.0f)) return HB_ERR_BAD_ARG;   // (2^60: no score overflows)
   const size_t need = hb_kv8_attention_scratch(c->cfg, r.n_rows, r.n_segs, r.max_keys, hb_kv8_min_split_keys());
   if (need > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 256))) return HB_ERR_BAD_ARG;
-  if (r.n_rows == 0 || r.n_segs == 0 || r.max_q_len == 0) return HB_OK;
+  if (r.n_rows == 0 || r.n_segs == 0) return HB_OK;   // (with a bound of zero rows the launch still reports segments beyond it)
   if (!q || !out) return HB_ERR_BAD_ARG;
   if (scale == 0.0f) scale = 1.0f / sqrtf(static_cast<float>(c->cfg.head_dim));
   int launches = 0;

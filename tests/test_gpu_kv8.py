@@ -684,6 +684,15 @@ def test_refusals():
     assert ctx.status_poll() == 0
 
 
+def test_rows_beyond_a_bound_of_zero_are_reported():
+    """A segment with rows where the call says that there are none, or keys where it says that there are none."""
+    ctx, kv, rows, q = _small()
+    for max_q_len, max_keys in ((0, 701), (20, 0), (0, 0)):
+        out = torch.full_like(q, -3.0)
+        ctx.kv8_attention(kv, 0, B.SegRows(rows.dev.segs, rows.dev.page_ids, rows.dev.row_seg, max_q_len, max_keys), q, out)
+        assert ctx.status_poll() == 2 and torch.all(out == -3.0), (max_q_len, max_keys)
+
+
 def test_nothing_to_do():
     cfg, ctx = context(8, 2, 64)
     kv = random_arena(cfg, 4, 0)
