@@ -51,13 +51,7 @@ __device__ __forceinline__ bool seg_ok(const Rows& r, int q_start, int q_len, in
          static_cast<long long>(pt_start) + pt_len <= r.n_page_ids && (keys + PAGE - 1) / PAGE <= pt_len;
 }
 
-// Two codes -> two fp16 (exact).
-__device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t two) {
-  uint32_t h;
-  asm("{\n\t.reg .b16 c;\n\tcvt.u16.u32 c, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, c;\n\t}" : "=r"(h) : "r"(two));
-  return h;
-}
-// Four codes: low two -> lo, high two -> hi.
+// Four codes -> four fp16 (exact): low two -> lo, high two -> hi.
 __device__ __forceinline__ void e4m3x4_to_half2x2(uint32_t w, uint32_t& lo, uint32_t& hi) {
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
       : "=r"(lo), "=r"(hi) : "r"(w));

@@ -138,7 +138,7 @@ __device__ __forceinline__ void load_gain(const __nv_bfloat16* gain, int d0, flo
   }
 }
 
-// Sixteen codes stored again under a scale 2^-shrink_log2 times as large (f = 2^(e_old - e_new) <= 1).
+// Sixteen codes again under a larger scale (f = old scale / new scale = 2^(e_old - e_new) <= 1).
 __device__ __forceinline__ uint4 rescale16(uint4 v, float f) {
   uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll

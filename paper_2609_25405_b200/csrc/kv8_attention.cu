@@ -295,7 +295,7 @@ __device__ __forceinline__ void page_step(const AttnParams& p, const Item& it, u
     }
   }
   // The reference maximum moves only when a column's maximum has grown by more than 2^13 over it.  It is
-  // kept 6 below the maximum it was taken from, so that P lies in (0, 2^15): the small probabilities of a
+  // kept 6 below the maximum it was taken from, so that P lies in [0, 2^13]: the small probabilities of a
   // long context stay normal fp16 numbers down to 2^-20 of the largest.
   if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
@@ -586,7 +586,7 @@ kv8_join_kernel(const AttnParams p) {
   constexpr int V = DH / 32;   // dimensions per lane
   for (int c = threadIdx.x >> 5; c < g.q_len * p.r.G; c += JOIN_WARPS) {
     const int64_t rec = record(p, seg, g, head, c);
-    // the splits' maxima and sums, up to four per lane
+    // the splits' maxima and sums, up to two per lane
     constexpr int N = MAX_SPLITS / 32;
     float2 ml[N];
     float m = -INFINITY;
