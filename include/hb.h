@@ -498,7 +498,8 @@ HB_API int hb_kv8_arena_bytes(const hb_model_cfg* cfg, int32_t n_pages, size_t* 
 /* hb_kv_create for the 8-bit format: an hb_kv whose pages are allocated, freed and destroyed with
  * the hb_kv_* calls above, and which hb_mixed_step[_lora] takes in place of a 16-bit cache (the
  * step's QKV projection then leaves fp16 rows for hb_kv8_append, and hb_kv8_attention reads the
- * pages).  Arena 256-byte aligned. */
+ * pages; its rows are rounded to fp16 before their rotation).  Such a step has at most 8192 segments.  Arena
+ * 256-byte aligned. */
 HB_API int hb_kv8_create(const hb_model_cfg* cfg, void* arena, size_t arena_bytes, int32_t n_pages, hb_kv** out);
 
 /* The rows of a step, in DEVICE memory the caller owns.  Of each segment q_start, q_len, pos_start,
@@ -557,8 +558,11 @@ HB_API int hb_kv8_append(hb_ctx* ctx, hb_kv* kv, int32_t layer, const hb_rows* r
  * a key makes the rows that see it NaN; a NaN in a value makes at least that dimension of them NaN
  * (the whole row where other rows of the segment come before the token).  Rows before the token
  * are not touched by it.  How a segment's keys are split depends on its own lengths only, never on
- * the rest of the batch.  (Inside hb_mixed_step the splits may be longer: there the context's limits
- * choose them.) */
+ * the rest of the batch.  Inside hb_mixed_step the splits may be longer than the 512 keys of this call: there
+ * they are 512 keys times the least power of two for which the records of max_segs requests of max_pos tokens fit
+ * into the context's activation buffer.  A context of 4096 rows of a 7B-class model has 512 up to 64 segments of 8192 positions,
+ * 4096 for 64 of 65552 and 32768 for 256 of 131072: with limits far beyond the requests, few long decode rows have too few
+ * splits to fill the GPU.  Scores beyond 2^20 in size are as coarse as fp32 is there, and an infinite q has no defined result. */
 HB_API int hb_kv8_attention_workspace(const hb_model_cfg* cfg, const hb_rows* rows, size_t* out_bytes);
 HB_API int hb_kv8_attention(hb_ctx* ctx, hb_kv* kv, int32_t layer, const hb_rows* rows, const void* q, int64_t q_stride,
                      void* out, int64_t out_stride, float scale, void* workspace, size_t workspace_bytes, void* stream);

@@ -760,7 +760,7 @@ class Context:
 
     def kv8_attention(self, kv, layer, rows, q, out, scale=0.0, stream=None):
         """hb_kv8_attention: causal attention of every row of `rows` over its request's pages of layer `layer` of a
-        KvCache8; q and out fp16 [T, Hq Dh] (rows may be strided views); scale 0 = 1 / sqrt(Dh).  The
+        KvCache8; q and out fp16 [T, Hq Dh] (rows may be strided views); scale 0 = 1 / sqrt(Dh), at most 2^60.  The
         workspace of the call comes from torch's allocator, on the stream of the call."""
         c = self.cfg
         T, dev = rows.struct.n_rows, self._same_device(rows, kv)

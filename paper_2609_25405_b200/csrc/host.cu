@@ -75,7 +75,8 @@ Layout make_layout(const hb_model_cfg& c, int32_t max_tokens, int32_t max_segs, 
   L.attn_out = cv.take(rows * n_q * 2);
   // act also holds what a step over an 8-bit cache needs between its QKV projection and its O projection: the
   // projection's fp16 rows, then (appended) the records of the decode splits.  A split there is as short as
-  // the records of max_segs requests of max_pos tokens allow; the context's limits decide, not the batch.
+  // the records of max_segs requests of max_pos tokens allow; the context's limits decide, not the batch.  (4096 rows of the
+  // 7B shape: 512 keys for 64 segments of 8192 positions, 4096 for 64 of 65552, 32768 for 256 of 131072.)
   const size_t n_qkv = n_q + 2ull * c.n_kv_heads * c.head_dim;
   const size_t act_bytes = rows * std::max<size_t>(c.d_ffn, n_qkv) * 2;
   L.act = cv.take(act_bytes);

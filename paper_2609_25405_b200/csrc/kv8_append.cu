@@ -18,7 +18,7 @@
 //     whole words of V, so that a page that starts afresh is written in words out of registers.  SHARE tasks
 //     look at the same 16 rows, find such leaders and share what they have to do (looking costs two
 //     dependent loads, so few look).  A page with fewer new rows goes to the query warps of its leader.
-//     4096 rows in 8 chunks, 32 / 8 heads of 128, norms and halves: 40 us = 2.35 TB/s (30.6 us without norms, in pairs;
+//     4096 rows in 8 chunks, 32 / 8 heads of 128, norms and halves: 40.7 us = 2.32 TB/s (30.6 us without norms, in pairs;
 //     26 where the pages begin with the rows).  No unit is full: the chain row, segment, page id, old scale and the
 //     rows themselves decides, with the 16 warps per SM that 128 registers allow.  16 heads a warp 41.6 us, and 21.6
 //     against 18.2 for 64 decode rows and 6 chunks; the rotary tables of both rows of a lane at once (spilled) 50.

@@ -18,10 +18,11 @@
 // The scale of K multiplies the fp32 scores.  The scale 2^e of V is folded into the exponent: P holds
 // 2^(s - m + e) with m the running maximum of s + e over the keys, and the sum takes 2^-e back out, so
 // neither scale is ever rounded.
-// Bound by HBM: 64 rows, 32 / 8 heads of 128, contexts of 512 to 4096 (300 MB) 63.2 us = 4.75 TB/s, ramp and tail
-// included; 256 rows at 2048 keys 195 us = 5.5 TB/s.  One row over 600 keys takes 9.6 us: the launches and one chain of
-// look-ups, pages and join.  Splits of at least 512 keys, at most 64 (128 of them for contexts of 64 Ki keys: 102 us
-// against 93, the join then reads twice the records).  Four blocks per SM with two pages per warp in flight: 63 us;
+// Bound by HBM: 64 rows, 32 / 8 heads of 128, contexts of 512 to 4096 (300 MB) 64.5 us = 4.65 TB/s, ramp and tail
+// included; 256 rows at 2048 keys 196 us = 5.5 TB/s.  The difference is the deal of the items: splits are equal within a segment
+// only, and with contexts that differ the fullest block has 1.30 times the mean (its SM 1.10 times).  One row over 600 keys takes
+// 10.1 us: the launches and one chain of look-ups, pages and join.  Splits of at least 512 keys, at most 64 (128 of them
+// for contexts of 64 Ki keys: 102 us against 93, the join then reads twice the records).  Four blocks per SM with two pages per warp in flight: 63 us;
 // three blocks with more stages 72; five (96 registers, spilled) 77.
 #include <algorithm>
 

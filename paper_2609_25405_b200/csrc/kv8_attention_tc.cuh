@@ -20,11 +20,11 @@
 // P, as in the decode body.  O is rescaled only when a row's maximum has grown by more than 2^8.
 // Bound by the two chains of dependent steps: 64 keys take a row tile about 2130 to 2420 cycles (scores 840 to 1110 until they
 // are there and 160 to read, maximum 370 to 400, exponentials and P 745 to 760), of which the tensor cores work 1090 for both
-// tiles together and the exponential unit 1020; tensor memory has no room for a third tile or a second S.  8 chunks of
-// 257 to 512 rows over 0 to 2048 earlier keys (74.5 GFLOP) 128 us = 580 TFLOP/s; one prompt of 4096 rows 176 us =
-// 780 TFLOP/s.  An item's start and end (look-up 1000 cycles, Q 4400, last P V 800, store 3600) weigh more on short
-// contexts.  Measured slower: Q and O through a stage in shared memory with whole lines, the next item's Q ahead (138 us);
-// Q_B in shared memory and two S per tile (150); two warps that issue MMAs (161); exponentials against the old
+// tiles together and the exponential unit 1020; with Q there tensor memory has no room for a third tile or a second S (Q in shared
+// memory and key tiles of 128 were not tried).  8 chunks of 257 to 512 rows over 0 to 2048 earlier keys (74.5 GFLOP) 130 us =
+// 574 TFLOP/s; one prompt of 4096 rows 180 us = 765 TFLOP/s; the chunks with heads of 64 109 us = 341 TFLOP/s.  An item's start and end (look-up 1000 cycles, Q 4400, last P V 800, store 3600) weigh more on short
+// contexts.  Measured slower: Q and O through a stage in shared memory with whole lines, the next item's Q ahead (138 us
+// against 128); Q_B in shared memory and two S per tile (150); two warps that issue MMAs (161); exponentials against the old
 // maximum while the new one is taken (131).
 // Every wait is bounded; on expiry the CTA raises a status bit, stores nothing more, frees its tensor memory
 // and leaves.
