@@ -303,7 +303,7 @@ HB_API int hb_argmax(hb_ctx* ctx, const float* logits, int32_t n_rows, int32_t* 
 
 /* Read (and clear) the device status word; synchronises `stream`.  0 = clean.
  * Non-zero: *out_code holds the OR of the bits below and the call returns
- * HB_ERR_DEVICE_STATUS.  Bits 0-5, 7 and 8 mean a kernel gave up (a bounded wait
+ * HB_ERR_DEVICE_STATUS.  Bits 0-5 and 7-11 mean a kernel gave up (a bounded wait
  * expired, an index check failed: outputs of that step are not valid); bit 6 is a
  * value report: the step ran, but an activation did not fit fp16. */
 enum {
@@ -315,6 +315,9 @@ enum {
   HB_STATUS_SELFTEST_WAIT = 32,   /* hb_selftest_wait_expiry                                  */
   HB_STATUS_TOKEN_INDEX = 128,    /* hb_logprobs: a token id beyond the vocabulary (its row got NaN) */
   HB_STATUS_LOGPROBS_WAIT = 256,  /* hb_logprobs: a pipeline wait expired                 */
+  HB_STATUS_ROW_INDEX = 512,      /* hb_quant_rows: an index beyond the source's rows (its row was not written) */
+  HB_STATUS_GROUP_INDEX = 1024,   /* hb_linear_grouped: bounds that decrease or pass the rows (that group was not computed) */
+  HB_STATUS_LINEAR_WAIT = 2048,   /* hb_linear, hb_linear_grouped: a pipeline wait expired */
   HB_STATUS_F16_RANGE = 64        /* a normed row or a SwiGLU output was NaN or beyond +-65504:
                                      finite values were stored saturated, NaN was stored as NaN */
 };
@@ -589,7 +592,7 @@ HB_API int hb_rope_table(int32_t n_pos, int32_t rot_dim, double theta, const hb_
 
 /* Largest number of alternatives hb_logprobs gives. */
 #define HB_LOGPROBS_MAX_K 32
-enum { HB_DTYPE_F32 = 0, HB_DTYPE_F16 = 1 };
+enum { HB_DTYPE_F32 = 0, HB_DTYPE_F16 = 1, HB_DTYPE_BF16 = 2, HB_DTYPE_E4M3 = 3 };   /* hb_logprobs takes the first two */
 
 /* Scores logits rows (the sampler's side of Algorithm 1: what hb_argmax decides, this measures).
  *   logits   device [n_rows, row_stride] of dtype, the first `vocab` of each row count; rows need no
@@ -606,6 +609,86 @@ enum { HB_DTYPE_F32 = 0, HB_DTYPE_F16 = 1 };
 HB_API int hb_logprobs(hb_ctx* ctx, const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride,
                 const int32_t* tokens, int32_t k, float* out_logprob, float* out_entropy, int32_t* out_top_ids,
                 float* out_top_logprobs, void* stream);
+
+/* ---- dense operators in 8 and 16 bits ------------------------------------------
+ *
+ * The projections of a layer with what stands around them, as calls of their own: the norm that
+ * feeds a product (hb_norm), rows brought to 8 bits (hb_quant_rows), and the product with scales,
+ * bias, activation and residual in its epilogue, with one weight (hb_linear) or one per run of rows
+ * (hb_linear_grouped).  Types are HB_DTYPE_*; strides are in elements and may exceed the row length.
+ * E4M3 rows carry one fp32 scale each, max(their largest magnitude, 2^-100) / 448: code c stands for
+ * c * scale.  A row that holds a NaN or an infinity has scale NaN and NaN codes.  fp16 outputs saturate at +-65504 (NaN stays NaN).  Nothing is allocated, and no call keeps
+ * anything for the next: calls of one context may run at the same time on different streams. */
+
+/* y = s / sqrt(mean(s^2) + eps) * gain with s = x (+ residual), one pass over the row.  Device pointers.
+ *   x         [n_rows, d] F32, F16 or BF16
+ *   residual  [n_rows, d] F32, F16 or BF16, or NULL
+ *   sum_out   [n_rows, d] of residual_dtype: s, rounded once (the norm takes the unrounded s); may be residual
+ *             itself; NULL if it is not wanted; without a residual it has to be NULL
+ *   gain      bf16 [d], or NULL = ones
+ *   y         [n_rows, d] F32, F16, BF16 or E4M3; may be x itself where type and stride are x's
+ *   y_scale   float [n_rows], E4M3 only (NULL otherwise)
+ * Pointers aligned to their type, 1 <= d <= HB_NORM_MAX_D; rows that start on 16-byte boundaries (8 for
+ * E4M3) with d a multiple of 8 are read and written in wide accesses.  Statistics in fp32. */
+#define HB_NORM_MAX_D 32768
+typedef struct {
+  const void* x;
+  const void* residual;
+  void* sum_out;
+  const void* gain;
+  void* y;
+  float* y_scale;
+  int64_t x_stride, residual_stride, sum_stride, y_stride;
+  int32_t x_dtype, residual_dtype, y_dtype;
+  int32_t n_rows, d;
+  float eps;
+} hb_norm_args;
+HB_API int hb_norm(hb_ctx* ctx, const hb_norm_args* args, void* stream);
+
+/* Rows to E4M3 with a scale each: row r of codes is row index[r] of x, or row r where index is NULL (then
+ * n_src >= n_rows).  x [n_src, d] F32, F16 or BF16; index device int32 [n_rows]: a negative entry leaves its row as
+ * it is, one >= n_src too and raises HB_STATUS_ROW_INDEX.  The same source row may be taken more than once.
+ * codes [n_rows, d], scale float [n_rows].  Limits and alignment as hb_norm's. */
+HB_API int hb_quant_rows(hb_ctx* ctx, const void* x, int32_t x_dtype, int64_t x_stride, int32_t n_src, const int32_t* index,
+                         int32_t n_rows, int32_t d, void* codes, int64_t codes_stride, float* scale, void* stream);
+
+/* Activations of hb_linear; GELU is x Phi(x), GELU_TANH its form with tanh. */
+enum { HB_ACT_NONE = 0, HB_ACT_RELU = 1, HB_ACT_SILU = 2, HB_ACT_GELU = 3, HB_ACT_GELU_TANH = 4 };
+
+/* C = act(z) + residual,  z[i, j] = a_scale[i] * w_scale[j] * sum_k a[i, k] * w[j, k] + bias[j]
+ * gated: w's rows are pairs (gate, up) as in hb_layer_weights.w_gate_up, C has n / 2 columns,
+ *        C[i, j] = act(z[i, 2j]) * z[i, 2j + 1] + residual[i, j].
+ *   a         [m, k] and w [n, k], both of ab_dtype: F16, BF16 or E4M3; 16-byte aligned, every row starts on a
+ *             16-byte boundary (k may be any)
+ *   a_scale   float [m] or NULL, w_scale float [n] or NULL (any ab_dtype), bias float [n] or NULL
+ *   residual  [m, columns of C] F32, F16 or BF16, or NULL; may be c itself where type and stride are c's
+ *   c         [m, n or n / 2] F32, F16 or BF16
+ * Device pointers.  Products are summed in fp32 on the tensor cores, everything after them in fp32, rounded once.
+ * The order of a sum depends on the sizes (m among them), never on values or timing: equal calls give equal bits. */
+typedef struct {
+  const void* a;
+  const void* w;
+  const float* a_scale;
+  const float* w_scale;
+  const float* bias;
+  const void* residual;
+  void* c;
+  int64_t a_stride, w_stride, residual_stride, c_stride;
+  int32_t m, n, k;
+  int32_t ab_dtype, c_dtype, residual_dtype;
+  int32_t act, gated;
+} hb_linear_args;
+HB_API int hb_linear(hb_ctx* ctx, const hb_linear_args* args, void* stream);
+
+/* hb_linear where rows group_start[g] .. group_start[g + 1] - 1 of a, c and residual take the g-th w, w_scale and
+ * bias: w [n_groups][n, k] with w_group_stride elements between them (a multiple of 16 bytes), w_scale and bias
+ * [n_groups, n].  Groups are an expert's rows, or the requests that share an adapter; a group may be empty.
+ * group_start: device int32 [n_groups + 1], not decreasing, in 0 .. m; read on the device only, so a captured call sees what
+ * it holds when it is replayed.  Rows before the first and behind the last group are left as they are.  A group that
+ * starts below an earlier bound, ends before it starts or leaves 0 .. m is skipped and raises HB_STATUS_GROUP_INDEX.  n_groups <= HB_LINEAR_MAX_GROUPS. */
+#define HB_LINEAR_MAX_GROUPS 512
+HB_API int hb_linear_grouped(hb_ctx* ctx, const hb_linear_args* args, const int32_t* group_start, int32_t n_groups,
+                             int64_t w_group_stride, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,8 @@ ERRORS = {0: "HB_OK", -1: "HB_ERR_BAD_ARG", -2: "HB_ERR_CUDA", -3: "HB_ERR_OOM_P
           -7: "HB_ERR_DEVICE_STATUS", -8: "HB_ERR_UNSUPPORTED"}
 from .consts import (KIND_DECODE, KIND_PREFILL_CHUNK, KIND_EMBED_CHUNK, POOL_NONE, POOL_MEAN,  # noqa: F401,E402
                      POOL_LAST, POOL_CLS, POOL_WMEAN, POOL_MAX, EPI_F16, EPI_F32, EPI_RESID_F32, EPI_SWIGLU, CLASSES,
-                     ROPE_PAIRS, ROPE_HALVES, ROPE_LINEAR, ROPE_BY_PARTS, LOGPROBS_MAX_K, DTYPE_F32, DTYPE_F16)
+                     ROPE_PAIRS, ROPE_HALVES, ROPE_LINEAR, ROPE_BY_PARTS, LOGPROBS_MAX_K, DTYPE_F32, DTYPE_F16, DTYPE_BF16, DTYPE_E4M3,
+                     ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH, NORM_MAX_D, LINEAR_MAX_GROUPS)
 
 
 class HbError(RuntimeError):
@@ -81,6 +82,18 @@ class RopeScaling(C.Structure):
                 ("hi", C.c_double), ("attn_factor", C.c_double)]
 
 
+class NormArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "residual", "sum_out", "gain", "y", "y_scale")] + \
+               [(n, C.c_int64) for n in ("x_stride", "residual_stride", "sum_stride", "y_stride")] + \
+               [(n, C.c_int32) for n in ("x_dtype", "residual_dtype", "y_dtype", "n_rows", "d")] + [("eps", C.c_float)]
+
+
+class LinearArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("a", "w", "a_scale", "w_scale", "bias", "residual", "c")] + \
+               [(n, C.c_int64) for n in ("a_stride", "w_stride", "residual_stride", "c_stride")] + \
+               [(n, C.c_int32) for n in ("m", "n", "k", "ab_dtype", "c_dtype", "residual_dtype", "act", "gated")]
+
+
 SEG_DTYPE = np.dtype([(n, np.int32) for n, _ in Seg._fields_])
 
 if not os.path.exists(LIB_PATH):
@@ -106,6 +119,10 @@ _sig = {
     "hb_kv8_attention": [_P, _P, C.c_int32, C.POINTER(RowsStruct), _P, C.c_int64, _P, C.c_int64, C.c_float, _P,
                          C.c_size_t, _P],
     "hb_logprobs": [_P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int64, _P, C.c_int32, _P, _P, _P, _P, _P],
+    "hb_norm": [_P, C.POINTER(NormArgs), _P],
+    "hb_quant_rows": [_P, _P, C.c_int32, C.c_int64, C.c_int32, _P, C.c_int32, C.c_int32, _P, C.c_int64, _P, _P],
+    "hb_linear": [_P, C.POINTER(LinearArgs), _P],
+    "hb_linear_grouped": [_P, C.POINTER(LinearArgs), _P, C.c_int32, C.c_int64, _P],
     "hb_rope_table": [C.c_int32, C.c_int32, C.c_double, C.POINTER(RopeScaling), _P, _P],
     "hb_pool_arena_bytes": [C.POINTER(ModelCfg), C.c_int32, C.POINTER(C.c_size_t)],
     "hb_pool_create": [C.POINTER(ModelCfg), _P, C.c_size_t, C.c_int32, C.POINTER(_P)],
@@ -570,6 +587,20 @@ def _rows_f16(t, rows, cols, device_index, name):
     raise ValueError(f"{name}: an fp16 tensor [{rows}, {cols}] with unit column stride on cuda:{device_index}")
 
 
+_DTYPES = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16, torch.float8_e4m3fn: DTYPE_E4M3}
+
+
+def _matrix(t, device_index, name):
+    """A matrix with unit column stride: (pointer, rows, columns, row stride, HB_DTYPE_*)."""
+    code = _DTYPES.get(t.dtype)
+    if code is not None and t.get_device() == device_index and t.dim() == 2:
+        rows, cols = t.shape
+        stride, unit = t.stride()
+        if unit == 1 or cols == 1 or rows * cols == 0:
+            return t.data_ptr(), rows, cols, (stride if rows > 1 else (cols + 15) // 16 * 16), code   # (one row: any stride)
+    raise ValueError(f"{name}: an fp32, fp16, bf16 or e4m3 matrix with unit column stride on cuda:{device_index}")
+
+
 class Pool:
     """Caller-owned pooling arena (torch) + the library's slot free list."""
 
@@ -706,6 +737,89 @@ class Context:
         if t.dtype is not dtype or t.get_device() != self.index or t.dim() > 2 or t.size(0) != n or t.numel() != n * k or not t.is_contiguous():
             raise ValueError(f"{name}: a contiguous {dtype} tensor of {n} x {k} on {self.device}")
         return t.data_ptr()
+
+    def norm(self, x, gain, y, residual=None, sum_out=None, y_scale=None, eps=None, stream=None):
+        """hb_norm: y = rmsnorm(x + residual) * gain over rows [n, d] (fp32, fp16 or bf16; y also float8_e4m3fn with
+        y_scale fp32 [n]).  gain bf16 [d] or None; sum_out takes x + residual in the residual's type (it may be the residual);
+        eps: None = the model's."""
+        dev = self.index
+        xp, n, d, xs, xt = _matrix(x, dev, "x")
+        yp, yn, yd, ys, yt = _matrix(y, dev, "y")
+        rp = sp = None
+        rs = ss = rt = 0
+        if (yn, yd) != (n, d):
+            raise ValueError(f"y: {n} x {d}, as x")
+        if residual is not None:
+            rp, rn, rd, rs, rt = _matrix(residual, dev, "residual")
+            if (rn, rd) != (n, d):
+                raise ValueError(f"residual: {n} x {d}, as x")
+        if sum_out is not None:
+            sp, sn, sd, ss, st = _matrix(sum_out, dev, "sum_out")
+            if residual is None or (sn, sd, st) != (n, d, rt):
+                raise ValueError(f"sum_out: {n} x {d} of the residual's type, with a residual")
+        a = NormArgs(xp, rp, sp, self._vector(gain, torch.bfloat16, d, 1, "gain"), yp,
+                     self._vector(y_scale, torch.float32, n, 1, "y_scale"), xs, rs, ss, ys, xt, rt, yt, n, d,
+                     self.cfg.rms_eps if eps is None else eps)
+        rc = lib.hb_norm(self.handle, C.byref(a), _stream_of(stream, dev))
+        if rc != HB_OK:
+            raise HbError(rc, "hb_norm")
+
+    def quant_rows(self, x, codes, scale, index=None, stream=None):
+        """hb_quant_rows: codes float8_e4m3fn [n, d] and scale fp32 [n] of the rows of x (fp32, fp16 or bf16), in order or row
+        index[r] (int32 [n]; negative leaves row r as it is)."""
+        dev = self.index
+        xp, n_src, d, xs, xt = _matrix(x, dev, "x")
+        cp, n, cd, cs, ct = _matrix(codes, dev, "codes")
+        if cd != d or ct != DTYPE_E4M3 or (index is None and n != n_src):
+            raise ValueError(f"codes: float8_e4m3fn, {d} columns and a row for each row of x or entry of index")
+        rc = lib.hb_quant_rows(self.handle, xp, xt, xs, n_src, self._vector(index, torch.int32, n, 1, "index"), n, d, cp, cs,
+                               self._vector(scale, torch.float32, n, 1, "scale"), _stream_of(stream, dev))
+        if rc != HB_OK:
+            raise HbError(rc, "hb_quant_rows")
+
+    def _linear_args(self, a, wp, n, k, ws, wt, per_column, out, a_scale, w_scale, bias, act, gated, residual):
+        dev = self.index
+        ap, m, ka, as_, at = _matrix(a, dev, "a")
+        cp, cm, cn, cs, ct = _matrix(out, dev, "out")
+        if ka != k or at != wt:
+            raise ValueError(f"a: {k} columns of the weight's type")
+        if cm != m or cn != (n // 2 if gated else n):
+            raise ValueError(f"out: {m} x {n // 2 if gated else n}")
+        rp, rs, rt = None, 0, 0
+        if residual is not None:
+            rp, rm, rn, rs, rt = _matrix(residual, dev, "residual")
+            if (rm, rn) != (cm, cn):
+                raise ValueError(f"residual: {cm} x {cn}, as out")
+        return LinearArgs(ap, wp, self._vector(a_scale, torch.float32, m, 1, "a_scale"),
+                          self._vector(w_scale, torch.float32, *per_column, "w_scale"),
+                          self._vector(bias, torch.float32, *per_column, "bias"), rp, cp, as_, ws, rs, cs, m, n, k, wt, ct, rt, act,
+                          1 if gated else 0)
+
+    def linear(self, a, w, out, a_scale=None, w_scale=None, bias=None, act=ACT_NONE, gated=False, residual=None, stream=None):
+        """hb_linear: out = act(a_scale w_scale a w^T + bias) + residual.  a [m, k] and w [n, k] of one type (fp16, bf16 or
+        float8_e4m3fn, rows on 16-byte boundaries), out and residual fp32, fp16 or bf16 [m, n], or [m, n / 2] where `gated`
+        joins pairs of columns; a_scale fp32 [m], w_scale and bias fp32 [n]."""
+        wp, n, k, ws, wt = _matrix(w, self.index, "w")
+        args = self._linear_args(a, wp, n, k, ws, wt, (n, 1), out, a_scale, w_scale, bias, act, gated, residual)
+        rc = lib.hb_linear(self.handle, C.byref(args), _stream_of(stream, self.index))
+        if rc != HB_OK:
+            raise HbError(rc, "hb_linear")
+
+    def linear_grouped(self, a, w, group_start, out, a_scale=None, w_scale=None, bias=None, act=ACT_NONE, gated=False,
+                       residual=None, stream=None):
+        """hb_linear_grouped: linear() where rows group_start[g] .. group_start[g + 1] - 1 take w[g]: w [groups, n, k],
+        group_start int32 [groups + 1] on the device, w_scale and bias fp32 [groups, n]."""
+        if w.dim() != 3 or w.shape[0] < 1:
+            raise ValueError("w: [groups, n, k]")
+        groups = w.shape[0]
+        wp, n, k, ws, wt = _matrix(w[0], self.index, "w")
+        args = self._linear_args(a, wp, n, k, ws, wt, (groups, n), out, a_scale, w_scale, bias, act, gated, residual)
+        if group_start is None:
+            raise ValueError("group_start: int32 [groups + 1]")
+        rc = lib.hb_linear_grouped(self.handle, C.byref(args), self._vector(group_start, torch.int32, groups + 1, 1, "group_start"),
+                                   groups, w.stride(0) if groups > 1 else n * ws, _stream_of(stream, self.index))
+        if rc != HB_OK:
+            raise HbError(rc, "hb_linear_grouped")
 
     def gemm_pair(self, A, B, A2, B2, Cout, M, N, K, K2, epilogue, stream=None):
         check(lib.hb_gemm_pair(self.handle, C.c_void_p(A.data_ptr()), C.c_void_p(B.data_ptr()),

@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhb.so")
 SOURCES = ["host.cu", "gemm_tcgen05.cu", "elementwise.cu", "attention.cu", "pool_static.cu", "kv8_append.cu", "kv8_attention.cu",
-           "logprobs.cu"]
+           "logprobs.cu", "rownorm.cu", "linear.cu"]
 
 
 def _stale():

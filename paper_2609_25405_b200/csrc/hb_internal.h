@@ -25,6 +25,9 @@ enum : uint32_t {
   HB_DEV_SELFTEST_WAIT_EXPIRED = 1u << 5,
   HB_DEV_TOKEN_BAD_INDEX = 1u << 7,
   HB_DEV_LOGPROBS_WAIT_EXPIRED = 1u << 8,
+  HB_DEV_ROW_BAD_INDEX = 1u << 9,
+  HB_DEV_GROUP_BAD_INDEX = 1u << 10,
+  HB_DEV_LINEAR_WAIT_EXPIRED = 1u << 11,
   HB_DEV_F16_RANGE = 1u << 6,   // a normed row or a SwiGLU output was NaN or beyond the largest finite half
 };
 
@@ -224,6 +227,14 @@ int hb_launch_wait_expiry_selftest(hb_ctx* c, uint64_t limit_ns, cudaStream_t s)
 int hb_launch_pool_chunk(hb_ctx* c, const float* x, const void* gain, int n_rows, int mode, int first_chunk,
                          int is_final, float* slot_sum, uint32_t* slot_meta, float* out_emb, cudaStream_t s);
 int hb_launch_bf16_to_f16(const void* src, void* dst, size_t n, cudaStream_t s);
+
+// dense operators (rownorm.cu, linear.cu); arguments already checked
+int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl);
+int hb_launch_quant_rows(hb_ctx* c, const void* x, int x_dtype, int64_t x_stride, int n_src, const int32_t* index, int n_rows, int d,
+                         void* codes, int64_t codes_stride, float* scale, cudaStream_t s, bool pdl);
+// group_start NULL: one group of all rows
+int hb_launch_linear(hb_ctx* c, const hb_linear_args& l, const int32_t* group_start, int n_groups, int64_t w_group_stride,
+                     cudaStream_t s, bool pdl);
 
 // 8-bit KV cache (kv8_append.cu, kv8_attention.cu)
 namespace hb_kv8 { struct Rows; }
