@@ -659,6 +659,20 @@ int hb_tmap_2d_f16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t c
   return r == CUDA_SUCCESS ? HB_OK : HB_ERR_CUDA;
 }
 
+int hb_tmap_bytes(CUtensorMap* out, const void* base, uint64_t inner, uint64_t rows, uint64_t planes, uint64_t row_stride,
+                  uint64_t plane_stride, uint32_t box_inner, uint32_t box_rows) {
+  EncodeTiledFn enc = get_encode_fn();
+  if (!enc) return HB_ERR_CUDA;
+  const cuuint64_t dims[3] = {inner, rows, planes};
+  const cuuint64_t strides[2] = {row_stride, plane_stride};
+  const cuuint32_t box[3] = {box_inner, box_rows, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, planes ? 3 : 2, const_cast<void*>(base), dims, strides, box, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? HB_OK : HB_ERR_CUDA;
+}
+
 // Tile width: 256 columns halves the shared-memory traffic per flop; 128 gives more tiles
 // when the problem has too few to fill the SMs or the last wave would be mostly idle.
 int hb_gemm_pick_bn(int M, int N, int num_sms) {

@@ -150,6 +150,11 @@ struct GemmArgs {
 int hb_tmap_2d_f16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols,
                    uint32_t box_rows);
 
+// The same over bytes: rows of `inner` bytes `row_stride` apart and, with planes > 0, planes of rows `plane_stride` apart; what
+// lies outside reads as zero.
+int hb_tmap_bytes(CUtensorMap* out, const void* base, uint64_t inner, uint64_t rows, uint64_t planes, uint64_t row_stride,
+                  uint64_t plane_stride, uint32_t box_inner, uint32_t box_rows);
+
 // Dynamic shared memory above 48 KiB has to be enabled per kernel ON EVERY DEVICE the kernel runs
 // on.  One of these per kernel instantiation remembers, per device, the largest size enabled so
 // far; hb_ensure_dyn_smem raises it on the current device when a launch needs more.  Threads that launch the
