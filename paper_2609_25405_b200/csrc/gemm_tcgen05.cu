@@ -673,6 +673,21 @@ int hb_tmap_bytes(CUtensorMap* out, const void* base, uint64_t inner, uint64_t r
   return r == CUDA_SUCCESS ? HB_OK : HB_ERR_CUDA;
 }
 
+int hb_tmap_block(CUtensorMap* out, const void* base, int dtype, uint64_t cols, uint64_t rows, uint64_t row_stride, uint32_t box_cols,
+                  uint32_t box_rows) {
+  EncodeTiledFn enc = get_encode_fn();
+  if (!enc) return HB_ERR_CUDA;
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {row_stride};
+  const cuuint32_t box[2] = {box_cols, box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUtensorMapDataType type = dtype == HB_DTYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == HB_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  const CUresult r = enc(out, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? HB_OK : HB_ERR_CUDA;
+}
+
 // Tile width: 256 columns halves the shared-memory traffic per flop; 128 gives more tiles
 // when the problem has too few to fill the SMs or the last wave would be mostly idle.
 int hb_gemm_pick_bn(int M, int N, int num_sms) {

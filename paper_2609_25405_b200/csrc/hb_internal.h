@@ -155,6 +155,10 @@ int hb_tmap_2d_f16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t c
 int hb_tmap_bytes(CUtensorMap* out, const void* base, uint64_t inner, uint64_t rows, uint64_t planes, uint64_t row_stride,
                   uint64_t plane_stride, uint32_t box_inner, uint32_t box_rows);
 
+// Boxes of an fp32, fp16 or bf16 matrix (HB_DTYPE_*), not swizzled; row_stride in bytes.
+int hb_tmap_block(CUtensorMap* out, const void* base, int dtype, uint64_t cols, uint64_t rows, uint64_t row_stride, uint32_t box_cols,
+                  uint32_t box_rows);
+
 // Dynamic shared memory above 48 KiB has to be enabled per kernel ON EVERY DEVICE the kernel runs
 // on.  One of these per kernel instantiation remembers, per device, the largest size enabled so
 // far; hb_ensure_dyn_smem raises it on the current device when a launch needs more.  Threads that launch the
