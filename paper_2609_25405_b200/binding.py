@@ -6,6 +6,7 @@ and raises if it has not been built -- there is no fallback of any kind.
 """
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -588,17 +589,34 @@ def _rows_f16(t, rows, cols, device_index, name):
 
 
 _DTYPES = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16, torch.float8_e4m3fn: DTYPE_E4M3}
+# The argument structs of the dense operators as bytes, and the calls that take them so: building a ctypes structure costs
+# more than a small kernel runs.
+_pack_norm = struct.Struct("6Q4q5if").pack
+_pack_linear = struct.Struct("7Q4q8i").pack
+_dense = C.CDLL(LIB_PATH)
+_dense.hb_norm.argtypes = [_P, C.c_char_p, _P]
+_dense.hb_linear.argtypes = [_P, C.c_char_p, _P]
+_dense.hb_linear_grouped.argtypes = [_P, C.c_char_p, _P, C.c_int32, C.c_int64, _P]
 
 
 def _matrix(t, device_index, name):
     """A matrix with unit column stride: (pointer, rows, columns, row stride, HB_DTYPE_*)."""
-    code = _DTYPES.get(t.dtype)
-    if code is not None and t.get_device() == device_index and t.dim() == 2:
-        rows, cols = t.shape
+    shape = t.shape
+    if len(shape) == 2 and t.get_device() == device_index and t.dtype in _DTYPES:
+        rows, cols = shape
         stride, unit = t.stride()
-        if unit == 1 or cols == 1 or rows * cols == 0:
-            return t.data_ptr(), rows, cols, (stride if rows > 1 else (cols + 15) // 16 * 16), code   # (one row: any stride)
+        if unit == 1 or cols == 1 or rows == 0 or cols == 0:
+            return t.data_ptr(), rows, cols, (stride if rows > 1 else (cols + 15) // 16 * 16), _DTYPES[t.dtype]   # (one row: any stride)
     raise ValueError(f"{name}: an fp32, fp16, bf16 or e4m3 matrix with unit column stride on cuda:{device_index}")
+
+
+def _packed(t, dtype, shape, device_index, name):
+    """Pointer of a contiguous tensor of that shape, 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device_index or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor {list(shape)} on cuda:{device_index}")
+    return t.data_ptr()
 
 
 class Pool:
@@ -745,23 +763,25 @@ class Context:
         dev = self.index
         xp, n, d, xs, xt = _matrix(x, dev, "x")
         yp, yn, yd, ys, yt = _matrix(y, dev, "y")
-        rp = sp = None
-        rs = ss = rt = 0
-        if (yn, yd) != (n, d):
+        if yn != n or yd != d:
             raise ValueError(f"y: {n} x {d}, as x")
+        rp = sp = rs = ss = rt = 0
         if residual is not None:
             rp, rn, rd, rs, rt = _matrix(residual, dev, "residual")
-            if (rn, rd) != (n, d):
+            if rn != n or rd != d:
                 raise ValueError(f"residual: {n} x {d}, as x")
         if sum_out is not None:
-            sp, sn, sd, ss, st = _matrix(sum_out, dev, "sum_out")
-            if residual is None or (sn, sd, st) != (n, d, rt):
-                raise ValueError(f"sum_out: {n} x {d} of the residual's type, with a residual")
-        a = NormArgs(xp, rp, sp, self._vector(gain, torch.bfloat16, d, 1, "gain"), yp,
-                     self._vector(y_scale, torch.float32, n, 1, "y_scale"), xs, rs, ss, ys, xt, rt, yt, n, d,
-                     self.cfg.rms_eps if eps is None else eps)
-        rc = lib.hb_norm(self.handle, C.byref(a), _stream_of(stream, dev))
-        if rc != HB_OK:
+            if sum_out is residual:
+                sp, ss = rp, rs
+            else:
+                sp, sn, sd, ss, st = _matrix(sum_out, dev, "sum_out")
+                if residual is None or sn != n or sd != d or st != rt:
+                    raise ValueError(f"sum_out: {n} x {d} of the residual's type, with a residual")
+        args = _pack_norm(xp, rp, sp, _packed(gain, torch.bfloat16, (d,), dev, "gain"), yp,
+                          _packed(y_scale, torch.float32, (n,), dev, "y_scale"), xs, rs, ss, ys, xt, rt, yt, n, d,
+                          self.cfg.rms_eps if eps is None else eps)
+        rc = _dense.hb_norm(self.handle, args, _stream_of(stream, dev))
+        if rc:
             raise HbError(rc, "hb_norm")
 
     def quant_rows(self, x, codes, scale, index=None, stream=None):
@@ -772,9 +792,9 @@ class Context:
         cp, n, cd, cs, ct = _matrix(codes, dev, "codes")
         if cd != d or ct != DTYPE_E4M3 or (index is None and n != n_src):
             raise ValueError(f"codes: float8_e4m3fn, {d} columns and a row for each row of x or entry of index")
-        rc = lib.hb_quant_rows(self.handle, xp, xt, xs, n_src, self._vector(index, torch.int32, n, 1, "index"), n, d, cp, cs,
-                               self._vector(scale, torch.float32, n, 1, "scale"), _stream_of(stream, dev))
-        if rc != HB_OK:
+        rc = lib.hb_quant_rows(self.handle, xp, xt, xs, n_src, _packed(index, torch.int32, (n,), dev, "index"), n, d, cp, cs,
+                               _packed(scale, torch.float32, (n,), dev, "scale"), _stream_of(stream, dev))
+        if rc:
             raise HbError(rc, "hb_quant_rows")
 
     def _linear_args(self, a, wp, n, k, ws, wt, per_column, out, a_scale, w_scale, bias, act, gated, residual):
@@ -785,40 +805,45 @@ class Context:
             raise ValueError(f"a: {k} columns of the weight's type")
         if cm != m or cn != (n // 2 if gated else n):
             raise ValueError(f"out: {m} x {n // 2 if gated else n}")
-        rp, rs, rt = None, 0, 0
+        rp = rs = rt = 0
         if residual is not None:
             rp, rm, rn, rs, rt = _matrix(residual, dev, "residual")
-            if (rm, rn) != (cm, cn):
+            if rm != cm or rn != cn:
                 raise ValueError(f"residual: {cm} x {cn}, as out")
-        return LinearArgs(ap, wp, self._vector(a_scale, torch.float32, m, 1, "a_scale"),
-                          self._vector(w_scale, torch.float32, *per_column, "w_scale"),
-                          self._vector(bias, torch.float32, *per_column, "bias"), rp, cp, as_, ws, rs, cs, m, n, k, wt, ct, rt, act,
-                          1 if gated else 0)
+        return _pack_linear(ap, wp, _packed(a_scale, torch.float32, (m,), dev, "a_scale"),
+                            _packed(w_scale, torch.float32, per_column, dev, "w_scale"),
+                            _packed(bias, torch.float32, per_column, dev, "bias"), rp, cp, as_, ws, rs, cs, m, n, k, wt, ct, rt, act,
+                            1 if gated else 0)
 
     def linear(self, a, w, out, a_scale=None, w_scale=None, bias=None, act=ACT_NONE, gated=False, residual=None, stream=None):
         """hb_linear: out = act(a_scale w_scale a w^T + bias) + residual.  a [m, k] and w [n, k] of one type (fp16, bf16 or
         float8_e4m3fn, rows on 16-byte boundaries), out and residual fp32, fp16 or bf16 [m, n], or [m, n / 2] where `gated`
         joins pairs of columns; a_scale fp32 [m], w_scale and bias fp32 [n]."""
         wp, n, k, ws, wt = _matrix(w, self.index, "w")
-        args = self._linear_args(a, wp, n, k, ws, wt, (n, 1), out, a_scale, w_scale, bias, act, gated, residual)
-        rc = lib.hb_linear(self.handle, C.byref(args), _stream_of(stream, self.index))
-        if rc != HB_OK:
+        args = self._linear_args(a, wp, n, k, ws, wt, (n,), out, a_scale, w_scale, bias, act, gated, residual)
+        rc = _dense.hb_linear(self.handle, args, _stream_of(stream, self.index))
+        if rc:
             raise HbError(rc, "hb_linear")
 
     def linear_grouped(self, a, w, group_start, out, a_scale=None, w_scale=None, bias=None, act=ACT_NONE, gated=False,
                        residual=None, stream=None):
         """hb_linear_grouped: linear() where rows group_start[g] .. group_start[g + 1] - 1 take w[g]: w [groups, n, k],
         group_start int32 [groups + 1] on the device, w_scale and bias fp32 [groups, n]."""
-        if w.dim() != 3 or w.shape[0] < 1:
-            raise ValueError("w: [groups, n, k]")
-        groups = w.shape[0]
-        wp, n, k, ws, wt = _matrix(w[0], self.index, "w")
-        args = self._linear_args(a, wp, n, k, ws, wt, (groups, n), out, a_scale, w_scale, bias, act, gated, residual)
+        shape, dev = w.shape, self.index
+        if len(shape) != 3 or shape[0] < 1 or w.dtype not in _DTYPES or w.get_device() != dev:
+            raise ValueError(f"w: fp16, bf16 or e4m3 [groups, n, k] on cuda:{dev}")
+        groups, n, k = shape
+        step, ws, unit = w.stride()
+        if unit != 1 and k > 1:
+            raise ValueError("w: unit stride along k")
+        if n == 1:
+            ws = (k + 15) // 16 * 16
         if group_start is None:
             raise ValueError("group_start: int32 [groups + 1]")
-        rc = lib.hb_linear_grouped(self.handle, C.byref(args), self._vector(group_start, torch.int32, groups + 1, 1, "group_start"),
-                                   groups, w.stride(0) if groups > 1 else n * ws, _stream_of(stream, self.index))
-        if rc != HB_OK:
+        args = self._linear_args(a, w.data_ptr(), n, k, ws, _DTYPES[w.dtype], (groups, n), out, a_scale, w_scale, bias, act, gated, residual)
+        rc = _dense.hb_linear_grouped(self.handle, args, _packed(group_start, torch.int32, (groups + 1,), dev, "group_start"),
+                                      groups, step if groups > 1 else n * ws, _stream_of(stream, dev))
+        if rc:
             raise HbError(rc, "hb_linear_grouped")
 
     def gemm_pair(self, A, B, A2, B2, Cout, M, N, K, K2, epilogue, stream=None):
