@@ -8,6 +8,8 @@
 // come out of ONE reduction and an 8-bit output needs no second pass over the row.
 #include <cuda_fp8.h>
 
+#include <initializer_list>
+
 #include "hb_internal.h"
 #include "ptx.cuh"
 
@@ -25,16 +27,13 @@ struct RowArgs {
   int64_t x_stride, res_stride, sum_stride, y_stride;
   int32_t n_rows, n_src, d;
   int32_t x_bf16, res_bf16, y_dtype;
+  int32_t lead0, lead_step;   // elements between a 16-byte boundary and the start of row r: (lead0 + r lead_step) mod 8
   float eps;
 };
 
 __device__ __forceinline__ float from16(uint32_t bits16, int bf16) {
   return bf16 ? __uint_as_float(bits16 << 16) : __half2float(__ushort_as_half(static_cast<unsigned short>(bits16)));
 }
-__device__ __forceinline__ uint32_t to16(float v, int bf16) {
-  return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(sat_half_range(v)));
-}
-__device__ __forceinline__ uint32_t to_e4m3(float v) { return __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
 
 // E consecutive elements of BYTES each, as loaded.
 template <int E, int BYTES>
@@ -55,13 +54,64 @@ struct Raw {
       w[0] = *reinterpret_cast<const unsigned short*>(p);
     }
   }
+  // the elements that lie in 0 .. d - 1 one by one
+  __device__ __forceinline__ void load_some(const void* row, int at, int d) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = 0u;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      if (at + j < 0 || at + j >= d) continue;
+      if constexpr (BYTES == 4) w[j] = static_cast<const uint32_t*>(row)[at + j];
+      else w[j / 2] |= static_cast<uint32_t>(static_cast<const unsigned short*>(row)[at + j]) << (16 * (j & 1));
+    }
+  }
   __device__ __forceinline__ float get(int i, int bf16) const {
     if constexpr (BYTES == 4) return __uint_as_float(w[i]);
     else return from16((w[i / 2] >> (16 * (i & 1))) & 0xffffu, bf16);
   }
 };
 
-// One row per T threads, NV vectors of E elements a thread (E = 8: wide accesses, E = 1: rows at any alignment).
+// Stores E values of a row from element `at` on, in one access or (some) those that lie in 0 .. d - 1 one by one.
+template <int E>
+__device__ __forceinline__ void put(void* row, int64_t at, int dtype, bool whole, int d, const float (&v)[E]) {
+  if constexpr (E == 8) {
+    if (whole) {
+      if (dtype == HB_DTYPE_E4M3) {
+        uint32_t w[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * j], v[4 * j + 1]), __NV_SATFINITE, __NV_E4M3);
+          const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * j + 2], v[4 * j + 3]), __NV_SATFINITE, __NV_E4M3);
+          w[j] = lo | static_cast<uint32_t>(hi) << 16;
+        }
+        *reinterpret_cast<uint2*>(static_cast<char*>(row) + at) = make_uint2(w[0], w[1]);
+      } else if (dtype == HB_DTYPE_F32) {
+        float4* o = reinterpret_cast<float4*>(static_cast<float*>(row) + at);
+        o[0] = make_float4(v[0], v[1], v[2], v[3]);
+        o[1] = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+        const bool bf16 = dtype == HB_DTYPE_BF16;
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = bf16 ? pack_bf16x2(v[2 * j], v[2 * j + 1]) : pack_f16x2_satfinite(v[2 * j], v[2 * j + 1]);
+        *reinterpret_cast<uint4*>(static_cast<unsigned short*>(row) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    if (at + j < 0 || at + j >= d) continue;
+    if (dtype == HB_DTYPE_E4M3) static_cast<unsigned char*>(row)[at + j] = __nv_cvt_float_to_fp8(v[j], __NV_SATFINITE, __NV_E4M3);
+    else if (dtype == HB_DTYPE_F32) static_cast<float*>(row)[at + j] = v[j];
+    else if (dtype == HB_DTYPE_BF16) static_cast<__nv_bfloat16*>(row)[at + j] = __float2bfloat16_rn(v[j]);
+    else static_cast<__half*>(row)[at + j] = __float2half_rn(sat_half_range(v[j]));
+  }
+}
+
+// One row per T threads, NV vectors of E elements a thread.  E = 8: wide accesses; vector v holds elements 8 v - lead .. 8 v - lead + 7,
+// where `lead` elements lie between a 16-byte boundary and the row's start, so that rows of any length stay wide but for their
+// first and last vector.  E = 1: rows whose arrays are not aligned alike.
 // XB / RB: bytes of an element of x and of the residual (0 = none).  NORM: false for hb_quant_rows.
 template <int XB, int RB, int T, int NV, int E, bool NORM>
 __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a) {
@@ -80,41 +130,48 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
     }
     src = i;
   }
+  const int lead = E == 8 ? static_cast<int>((a.lead0 + r * a.lead_step) & 7) : 0;
   const char* x = static_cast<const char*>(a.x) + src * a.x_stride * XB;
   const char* res = RB ? static_cast<const char*>(a.res) + r * a.res_stride * RB : nullptr;
+  auto first = [&](int i) { return (tid + i * T) * E - lead; };
+  auto some = [&](int at) { return at < a.d && at + E > 0; };          // any of the vector's elements exists
+  auto whole = [&](int at) { return at >= 0 && at + E <= a.d; };
   Raw<E, XB> rx[NV];
   Raw<E, RB ? RB : 4> rr[RB ? NV : 1];
   Raw<E, 2> rg[NORM ? NV : 1];
   const bool has_gain = NORM && a.gain;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int at = (tid + i * T) * E;
-    if (at < a.d) {
+    const int at = first(i);
+    if (whole(at)) {
       rx[i].load(x, at);
       if constexpr (RB != 0) rr[i].load(res, at);
-      if constexpr (NORM) {
-        if (has_gain) rg[i].load(a.gain, at);
+    } else {
+      rx[i].load_some(x, at, a.d);
+      if constexpr (RB != 0) rr[i].load_some(res, at, a.d);
+    }
+    if constexpr (NORM) {
+      if (has_gain) {
+        if (lead == 0 && whole(at)) rg[i].load(a.gain, at);
+        else rg[i].load_some(a.gain, at, a.d);
       }
     }
   }
-  float s[NV][E];
+  float s[NORM ? NV : 1][E];
   float ss = 0.0f;
   uint32_t top = 0u;   // largest magnitude as bits: their order is that of the values, and NaN comes out on top
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const bool in = (tid + i * T) * E < a.d;
 #pragma unroll
     for (int j = 0; j < E; ++j) {
       float v = rx[i].get(j, a.x_bf16);
       if constexpr (RB != 0) v += rr[i].get(j, a.res_bf16);
-      if (!in) v = 0.0f;
-      s[i][j] = v;
-      float w = v;
       if constexpr (NORM) {
+        s[i][j] = v;
         ss = fmaf(v, v, ss);
-        if (has_gain && in) w *= rg[i].get(j, 1);
+        if (has_gain) v *= rg[i].get(j, 1);
       }
-      top = max(top, __float_as_uint(w) & 0x7fffffffu);
+      top = max(top, __float_as_uint(v) & 0x7fffffffu);
     }
   }
   if constexpr (RB != 0) {
@@ -122,22 +179,8 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
       char* out = static_cast<char*>(a.sum) + r * a.sum_stride * RB;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int at = (tid + i * T) * E;
-        if (at < a.d) {
-          if constexpr (E == 1) {
-            if constexpr (RB == 4) reinterpret_cast<float*>(out)[at] = s[i][0];
-            else reinterpret_cast<unsigned short*>(out)[at] = static_cast<unsigned short>(to16(s[i][0], a.res_bf16));
-          } else if constexpr (RB == 4) {
-            float4* o = reinterpret_cast<float4*>(out + static_cast<size_t>(at) * 4);
-            o[0] = make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
-            o[1] = make_float4(s[i][4], s[i][5], s[i][6], s[i][7]);
-          } else {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = to16(s[i][2 * j], a.res_bf16) | to16(s[i][2 * j + 1], a.res_bf16) << 16;
-            *reinterpret_cast<uint4*>(out + static_cast<size_t>(at) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-        }
+        const int at = first(i);
+        if (some(at)) put<E>(out, at, RB == 4 ? HB_DTYPE_F32 : a.res_bf16 ? HB_DTYPE_BF16 : HB_DTYPE_F16, whole(at), a.d, s[i]);
       }
     }
   }
@@ -171,53 +214,23 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
     inv = finite ? 448.0f / m : __int_as_float(0x7fffffff);
     if (tid == 0) a.scale[r] = finite ? m / 448.0f : __int_as_float(0x7fffffff);
   }
+  char* y = static_cast<char*>(a.y) + r * a.y_stride * (a.y_dtype == HB_DTYPE_E4M3 ? 1 : a.y_dtype == HB_DTYPE_F32 ? 4 : 2);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int at = (tid + i * T) * E;
-    if (at >= a.d) continue;
+    const int at = first(i);
+    if (!some(at)) continue;
     float v[E];
 #pragma unroll
     for (int j = 0; j < E; ++j) {
-      v[j] = s[i][j];
       if constexpr (NORM) {
-        v[j] *= rstd;
+        v[j] = s[i][j] * rstd;
         if (has_gain) v[j] *= rg[i].get(j, 1);
+      } else {
+        v[j] = rx[i].get(j, a.x_bf16);     // (kept as loaded: half the registers)
       }
+      v[j] *= inv;
     }
-    if (a.y_dtype == HB_DTYPE_E4M3) {
-      char* y = static_cast<char*>(a.y) + r * a.y_stride + at;
-      if constexpr (E == 1) {
-        *y = static_cast<char>(to_e4m3(v[0] * inv));
-      } else {
-        uint32_t w[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * j] * inv, v[4 * j + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-          const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * j + 2] * inv, v[4 * j + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-          w[j] = lo | static_cast<uint32_t>(hi) << 16;
-        }
-        *reinterpret_cast<uint2*>(y) = make_uint2(w[0], w[1]);
-      }
-    } else if (a.y_dtype == HB_DTYPE_F32) {
-      float* y = static_cast<float*>(a.y) + r * a.y_stride + at;
-      if constexpr (E == 1) {
-        *y = v[0];
-      } else {
-        reinterpret_cast<float4*>(y)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(y)[1] = make_float4(v[4], v[5], v[6], v[7]);
-      }
-    } else {
-      const int bf16 = a.y_dtype == HB_DTYPE_BF16;
-      unsigned short* y = static_cast<unsigned short*>(a.y) + r * a.y_stride + at;
-      if constexpr (E == 1) {
-        *y = static_cast<unsigned short>(to16(v[0], bf16));
-      } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = to16(v[2 * j], bf16) | to16(v[2 * j + 1], bf16) << 16;
-        *reinterpret_cast<uint4*>(y) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
+    put<E>(y, at, a.y_dtype, whole(at), a.d, v);
   }
 }
 
@@ -227,21 +240,57 @@ int launch(const RowArgs& a, cudaStream_t s, bool pdl) {
   return hb_launch_kernel(row_kernel<XB, RB, T, NV, E, NORM>, grid, T == 32 ? 256 : T, 0, s, pdl, a);
 }
 
+// Threads of a row and vectors of a thread.  An SM needs some 40 KB under way: where a vector is few bytes (no residual), four a
+// thread reach that if there are enough rows (8192 fp16 to codes, 4096 rows: 18.9 us, with one or two a thread 27.7); otherwise
+// more threads do (4096 fp16 + fp32 to codes, 4096 rows: 28.9 us = 6.4 TB/s, 99 % of the copy rate).
 template <int XB, int RB, bool NORM>
-int launch_size(const RowArgs& a, bool wide, cudaStream_t s, bool pdl) {
+int launch_size(const RowArgs& a, bool wide, bool many, cudaStream_t s, bool pdl) {
   if (!wide) {
     if (a.d <= 256) return launch<XB, RB, 32, 8, 1, NORM>(a, s, pdl);
     if (a.d <= 2048) return launch<XB, RB, 256, 8, 1, NORM>(a, s, pdl);
     if (a.d <= 8192) return launch<XB, RB, 1024, 8, 1, NORM>(a, s, pdl);
     return launch<XB, RB, 1024, 32, 1, NORM>(a, s, pdl);
   }
-  if (a.d <= 256) return launch<XB, RB, 32, 1, 8, NORM>(a, s, pdl);
-  if (a.d <= 1024) return launch<XB, RB, 32, 4, 8, NORM>(a, s, pdl);
-  if (a.d <= 2048) return launch<XB, RB, 256, 1, 8, NORM>(a, s, pdl);
-  if (a.d <= 4096) return launch<XB, RB, 512, 1, 8, NORM>(a, s, pdl);
-  if (a.d <= 8192) return launch<XB, RB, 1024, 1, 8, NORM>(a, s, pdl);
-  if (a.d <= 16384) return launch<XB, RB, 1024, 2, 8, NORM>(a, s, pdl);
-  return launch<XB, RB, 1024, 4, 8, NORM>(a, s, pdl);
+  const int d = a.d + ((a.lead0 | a.lead_step) & 7 ? 7 : 0);     // with the elements in front of the row
+  if (d <= 256) return launch<XB, RB, 32, 1, 8, NORM>(a, s, pdl);
+  if (d <= 512) return launch<XB, RB, 32, 2, 8, NORM>(a, s, pdl);
+  if (d <= 1024) return launch<XB, RB, 32, 4, 8, NORM>(a, s, pdl);
+  if constexpr ((XB == 2 || !NORM) && RB == 0) {
+    if (many) {
+      if (d <= 2048) return launch<XB, RB, 64, 4, 8, NORM>(a, s, pdl);
+      if (d <= 4096) return launch<XB, RB, 128, 4, 8, NORM>(a, s, pdl);
+      if (d <= 8192) return launch<XB, RB, 256, 4, 8, NORM>(a, s, pdl);
+      if (d <= 16384) return launch<XB, RB, 512, 4, 8, NORM>(a, s, pdl);
+    }
+  }
+  if (d <= 2048) return launch<XB, RB, 256, 1, 8, NORM>(a, s, pdl);
+  if (d <= 4096) return launch<XB, RB, 512, 1, 8, NORM>(a, s, pdl);
+  if (d <= 8192) return launch<XB, RB, 512, 2, 8, NORM>(a, s, pdl);
+  if (d <= 16384) return launch<XB, RB, 1024, 2, 8, NORM>(a, s, pdl);
+  if (d <= 32768) return launch<XB, RB, 1024, 4, 8, NORM>(a, s, pdl);
+  return launch<XB, RB, 1024, 32, 1, NORM>(a, s, pdl);
+}
+
+// The rows of one array: first element, elements between rows, bytes of an element.
+struct Rows {
+  const void* p;
+  int64_t stride;
+  int size;
+};
+// Whether the arrays of a call are aligned alike, so that one `lead` per row serves them all: a wide access takes 8 elements of 1 or
+// 2 bytes from a boundary of as many, or 4 of 4 bytes.
+bool aligned_alike(std::initializer_list<Rows> arrays, RowArgs* a) {
+  const Rows* ref = arrays.begin();
+  for (const Rows& x : arrays)
+    if (x.p && x.size < 4) ref = &x;
+  const int64_t lead = reinterpret_cast<uintptr_t>(ref->p) / ref->size % 8, step = ref->stride % 8;
+  for (const Rows& x : arrays) {
+    const int64_t unit = x.size == 4 ? 4 : 8;
+    if (x.p && ((reinterpret_cast<uintptr_t>(x.p) / x.size) % unit != static_cast<uint64_t>(lead % unit) || x.stride % unit != step % unit)) return false;
+  }
+  a->lead0 = static_cast<int32_t>(lead);
+  a->lead_step = static_cast<int32_t>(step);
+  return true;
 }
 
 int elem_bytes(int dtype) { return dtype == HB_DTYPE_F32 ? 4 : dtype == HB_DTYPE_E4M3 ? 1 : 2; }
@@ -267,14 +316,15 @@ int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl) {
   a.n_rows = n.n_rows; a.n_src = n.n_rows; a.d = n.d;
   a.x_bf16 = n.x_dtype == HB_DTYPE_BF16; a.res_bf16 = n.residual_dtype == HB_DTYPE_BF16; a.y_dtype = n.y_dtype; a.eps = n.eps;
   const int xb = elem_bytes(n.x_dtype), rb = n.residual ? elem_bytes(n.residual_dtype) : 0, yb = elem_bytes(n.y_dtype);
-  const bool wide = n.d % 8 == 0 && rows_on(n.x, n.x_stride, xb, 16) && rows_on(n.gain, 0, 2, 16) && rows_on(n.y, n.y_stride, yb, yb == 1 ? 8 : 16) &&
-                    (!rb || (rows_on(n.residual, n.residual_stride, rb, 16) && rows_on(n.sum_out, n.sum_stride, rb, 16)));
+  const bool wide = rows_on(n.gain, 0, 2, 16) &&
+                    aligned_alike({{n.x, n.x_stride, xb}, {n.residual, n.residual_stride, rb ? rb : 1}, {n.sum_out, n.sum_stride, rb ? rb : 1}, {n.y, n.y_stride, yb}}, &a);
+  const bool many = n.n_rows >= 2 * c->num_sms;
   if (xb == 4) {
-    if (rb == 0) return launch_size<4, 0, true>(a, wide, s, pdl);
-    return rb == 4 ? launch_size<4, 4, true>(a, wide, s, pdl) : launch_size<4, 2, true>(a, wide, s, pdl);
+    if (rb == 0) return launch_size<4, 0, true>(a, wide, many, s, pdl);
+    return rb == 4 ? launch_size<4, 4, true>(a, wide, many, s, pdl) : launch_size<4, 2, true>(a, wide, many, s, pdl);
   }
-  if (rb == 0) return launch_size<2, 0, true>(a, wide, s, pdl);
-  return rb == 4 ? launch_size<2, 4, true>(a, wide, s, pdl) : launch_size<2, 2, true>(a, wide, s, pdl);
+  if (rb == 0) return launch_size<2, 0, true>(a, wide, many, s, pdl);
+  return rb == 4 ? launch_size<2, 4, true>(a, wide, many, s, pdl) : launch_size<2, 2, true>(a, wide, many, s, pdl);
 }
 
 int hb_launch_quant_rows(hb_ctx* c, const void* x, int x_dtype, int64_t x_stride, int n_src, const int32_t* index, int n_rows, int d,
@@ -285,8 +335,9 @@ int hb_launch_quant_rows(hb_ctx* c, const void* x, int x_dtype, int64_t x_stride
   a.n_rows = n_rows; a.n_src = n_src; a.d = d;
   a.x_bf16 = x_dtype == HB_DTYPE_BF16; a.y_dtype = HB_DTYPE_E4M3;
   const int xb = elem_bytes(x_dtype);
-  const bool wide = d % 8 == 0 && rows_on(x, x_stride, xb, 16) && rows_on(codes, codes_stride, 1, 8);
-  return xb == 4 ? launch_size<4, 0, false>(a, wide, s, pdl) : launch_size<2, 0, false>(a, wide, s, pdl);
+  const bool wide = aligned_alike({{x, x_stride, xb}, {codes, codes_stride, 1}}, &a) && (!index || a.lead_step == 0);   // (an index breaks the step)
+  const bool many = n_rows >= 2 * c->num_sms;
+  return xb == 4 ? launch_size<4, 0, false>(a, wide, many, s, pdl) : launch_size<2, 0, false>(a, wide, many, s, pdl);
 }
 
 extern "C" int hb_norm(hb_ctx* c, const hb_norm_args* n, void* stream) {
