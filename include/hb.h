@@ -690,6 +690,27 @@ HB_API int hb_linear(hb_ctx* ctx, const hb_linear_args* args, void* stream);
 HB_API int hb_linear_grouped(hb_ctx* ctx, const hb_linear_args* args, const int32_t* group_start, int32_t n_groups,
                              int64_t w_group_stride, void* stream);
 
+/* The step with 8-bit projection weights: hb_mixed_step over an 8-bit cache (hb_kv8_create) whose four projections per layer
+ * run on E4M3 operands.  Per layer: hb_norm to codes, hb_linear QKV, append and attention over the 8-bit cache,
+ * hb_quant_rows of the attention's output, hb_linear O onto the residual stream, hb_norm, hb_linear gate/up with SwiGLU,
+ * hb_quant_rows, hb_linear down onto the residual stream.  Embedding, gains, LM head, pooling and outputs are hb_mixed_step's.
+ * Every projection weight is E4M3 codes, row-major [out, in] in hb_layer_weights' row order, 16-byte aligned, with a float
+ * scale per row (hb_quant_rows of the model's rows gives both).  No adapters.  A row's projections depend on the number of
+ * rows of the step in their last bits (hb_linear), unlike hb_mixed_step's.  HB_STATUS_F16_RANGE is raised by the first norm only. */
+typedef struct {
+  const void *attn_norm, *ffn_norm;                 /* bf16 [d_model] */
+  const void *wqkv, *wo, *w_gate_up, *w_down;       /* E4M3 codes */
+  const float *wqkv_scale, *wo_scale, *gate_up_scale, *down_scale;
+} hb_layer_weights8;
+typedef struct {
+  const void* tok_emb;               /* device */
+  const hb_layer_weights8* layers;   /* HOST array [n_layers] of device ptrs   */
+  const void* final_norm;            /* device */
+  const void* lm_head;               /* device, fp16 */
+} hb_weights8;
+HB_API int hb_mixed_step8(hb_ctx* ctx, const hb_batch_desc* desc, const hb_weights8* w, hb_kv* kv, hb_pool* pool,
+                          float* out_logits, float* out_emb, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -46,6 +46,15 @@ class Weights(C.Structure):
                 ("final_norm", C.c_void_p), ("lm_head", C.c_void_p)]
 
 
+class LayerWeights8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("attn_norm", "ffn_norm", "wqkv", "wo", "w_gate_up", "w_down", "wqkv_scale", "wo_scale",
+                                          "gate_up_scale", "down_scale")]
+
+
+class Weights8(C.Structure):
+    _fields_ = [("tok_emb", C.c_void_p), ("layers", C.POINTER(LayerWeights8)), ("final_norm", C.c_void_p), ("lm_head", C.c_void_p)]
+
+
 class LoraLayer(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("a_qkv", "b_qkv", "a_o", "b_o", "a_gu", "b_gu", "a_d", "b_d")]
 
@@ -136,6 +145,7 @@ _sig = {
                          C.POINTER(BatchDesc)],
     "hb_mixed_step": [_P, C.POINTER(BatchDesc), C.POINTER(Weights), _P, _P, _P, _P, _P],
     "hb_mixed_step_lora": [_P, C.POINTER(BatchDesc), C.POINTER(Weights), C.POINTER(Lora), _P, _P, _P, _P, _P],
+    "hb_mixed_step8": [_P, C.POINTER(BatchDesc), C.POINTER(Weights8), _P, _P, _P, _P, _P],
     "hb_weights_pack_f16": [_P, _P, C.c_size_t, _P],
     "hb_argmax": [_P, _P, C.c_int32, _P, _P],
     "hb_pool_chunk": [_P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P, _P],
@@ -280,6 +290,71 @@ class DeviceWeights:
             lw.w_gate_up = rnd(2 * shape.F, shape.d)
             lw.w_down = rnd(shape.d, shape.F)
         return self
+
+
+class DeviceWeights8:
+    """Weights with the projections in 8 bits (e4m3 codes and a scale per row), plus the hb_weights8 struct; token embedding, gains
+    and LM head as in DeviceWeights.  About half the memory of DeviceWeights; for an Engine with kv_dtype="e4m3"."""
+
+    def __init__(self, n_layers, device="cuda"):
+        self.tensors = []          # keep-alive
+        self.layers = (LayerWeights8 * n_layers)()
+        self.struct = Weights8()
+        self.struct.layers = C.cast(self.layers, C.POINTER(LayerWeights8))
+        self.codes = [{} for _ in range(n_layers)]   # per layer: name -> (codes, scale)
+        self._device = device
+        self._ctx = Context(ModelCfg(1, 64, 1, 1, 64, 64, 64, 16, 64, 1e4, 1e-5), 1, 1, 1)   # quantises the rows
+
+    def _keep(self, t):
+        self.tensors.append(t)
+        return t.data_ptr()
+
+    def _set(self, layer, name, scale_name, w):
+        """Quantises the rows of w [out, in] (bf16, fp16 or fp32 on the device)."""
+        codes = torch.empty(w.shape, dtype=torch.float8_e4m3fn, device=w.device)
+        scale = torch.empty(w.shape[0], dtype=torch.float32, device=w.device)
+        self._ctx.quant_rows(w, codes, scale)
+        self.codes[layer][name] = (codes, scale)
+        setattr(self.layers[layer], name, self._keep(codes))
+        setattr(self.layers[layer], scale_name, self._keep(scale))
+
+    def _rest(self, tok_emb, final_norm, lm_head):
+        self.struct.tok_emb, self.struct.final_norm, self.struct.lm_head = (self._keep(t) for t in (tok_emb, final_norm, lm_head))
+        torch.cuda.synchronize()      # the rows' sources go when the caller's do
+        self._ctx.close()
+        return self
+
+    @classmethod
+    def from_synth(cls, W, device="cuda"):
+        """Upload synth.Weights: rows in DeviceWeights' order, quantised by the library."""
+        s = W.shape
+        self = cls(s.L, device)
+        up = lambda a: bf16_from_f32(a, device)   # noqa: E731
+        for l in range(s.L):
+            w = W.layer(l)
+            self.layers[l].attn_norm, self.layers[l].ffn_norm = self._keep(up(w["attn_norm"])), self._keep(up(w["ffn_norm"]))
+            gu = np.empty((2 * s.F, s.d), dtype=np.float32)
+            gu[0::2], gu[1::2] = w["wg"], w["wu"]
+            qkv = np.concatenate([rope_interleave_rows(w["wq"], s.Dh), rope_interleave_rows(w["wk"], s.Dh), w["wv"]], axis=0)
+            for name, scale, a in (("wqkv", "wqkv_scale", qkv), ("wo", "wo_scale", w["wo"]), ("w_gate_up", "gate_up_scale", gu),
+                                   ("w_down", "down_scale", w["wd"])):
+                self._set(l, name, scale, up(a))
+        return self._rest(up(W.tok_emb), up(W.final_norm), pack_f16_(up(W.lm_head)))
+
+    @classmethod
+    def random_on_device(cls, shape, seed=0, std=0.02, device="cuda"):
+        """N(0, std^2) weights drawn on the device (benchmarks)."""
+        self = cls(shape.L, device)
+        g = torch.Generator(device=device)
+        g.manual_seed(seed)
+        rnd = lambda r, c: torch.empty((r, c), dtype=torch.bfloat16, device=device).normal_(0.0, std, generator=g)   # noqa: E731
+        ones = lambda: torch.ones(shape.d, dtype=torch.bfloat16, device=device)   # noqa: E731
+        for l in range(shape.L):
+            self.layers[l].attn_norm, self.layers[l].ffn_norm = self._keep(ones()), self._keep(ones())
+            for name, scale, r, c in (("wqkv", "wqkv_scale", shape.n_qkv, shape.d), ("wo", "wo_scale", shape.d, shape.Hq * shape.Dh),
+                                      ("w_gate_up", "gate_up_scale", 2 * shape.F, shape.d), ("w_down", "down_scale", shape.d, shape.F)):
+                self._set(l, name, scale, rnd(r, c))
+        return self._rest(rnd(shape.V, shape.d), ones(), pack_f16_(rnd(shape.V, shape.d)))
 
 
 def _pad64(n):
@@ -715,7 +790,11 @@ class Context:
         tail = (kv.handle, pool.handle if pool is not None else None,
                 C.c_void_p(out_logits.data_ptr()) if out_logits is not None else None,
                 C.c_void_p(out_emb.data_ptr()) if out_emb is not None else None, _stream_ptr(stream))
-        if lora is None:
+        if isinstance(weights, DeviceWeights8):
+            if lora is not None or not isinstance(kv, KvCache8):
+                raise ValueError("8-bit weights: with an 8-bit cache (KvCache8) and without adapters")
+            check(lib.hb_mixed_step8(self.handle, C.byref(batch.desc), C.byref(weights.struct), *tail), "hb_mixed_step8")
+        elif lora is None:
             check(lib.hb_mixed_step(self.handle, C.byref(batch.desc), C.byref(weights.struct), *tail), "hb_mixed_step")
         else:
             check(lib.hb_mixed_step_lora(self.handle, C.byref(batch.desc), C.byref(weights.struct),

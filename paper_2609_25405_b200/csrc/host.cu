@@ -681,6 +681,48 @@ int hb_validate_desc(const hb_model_cfg* cfg, int32_t max_tokens, int32_t max_se
   return validate(*cfg, max_tokens, max_segs, max_page_ids, n_pages, n_slots, cfg->max_pos, desc, vs);
 }
 
+}  // extern "C"
+
+namespace {
+
+// One layer of the step up to the residual stream, with 8-bit projection weights (see hb_mixed_step8).
+struct Layer8 {
+  hb_ctx* c;
+  const hb_layer_weights8& w;
+  int T;
+  cudaStream_t s;
+  // one scale per row, in the buffer of the adapters' activations, which this step does not have
+  float* row_scale() const { return reinterpret_cast<float*>(c->lora_u); }
+  int norm(const void* gain) const {                        // x -> codes in h
+    hb_norm_args n = {};
+    n.x = c->x; n.gain = gain; n.y = c->h; n.y_scale = row_scale();
+    n.x_stride = n.y_stride = n.d = c->cfg.d_model;
+    n.x_dtype = HB_DTYPE_F32; n.y_dtype = HB_DTYPE_E4M3; n.n_rows = T; n.eps = c->cfg.rms_eps;
+    return hb_launch_norm(c, n, s, c->pdl);
+  }
+  // fp16 rows to codes in place: a row's codes take the first half of its bytes, and whoever writes them has read all of them
+  int codes(__half* x, int d) const {
+    return hb_launch_quant_rows(c, x, HB_DTYPE_F16, d, T, nullptr, T, d, x, 2 * d, row_scale(), s, c->pdl);
+  }
+  int project(const void* a, int a_stride, const void* weight, const float* scale, void* out, int n, int k, int dtype, bool residual, bool swiglu) const {
+    hb_linear_args l = {};
+    l.a = a; l.a_stride = a_stride; l.a_scale = row_scale();
+    l.w = weight; l.w_stride = k; l.w_scale = scale;
+    l.c = out; l.c_stride = swiglu ? n / 2 : n; l.c_dtype = dtype;
+    if (residual) { l.residual = out; l.residual_stride = n; l.residual_dtype = dtype; }
+    l.m = T; l.n = n; l.k = k; l.ab_dtype = HB_DTYPE_E4M3;
+    if (swiglu) { l.act = HB_ACT_SILU; l.gated = 1; }
+    return hb_launch_linear(c, l, nullptr, 1, 0, s, c->pdl);
+  }
+};
+
+int mixed_step(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, const hb_lora* lora, const hb_layer_weights8* layers8, hb_kv* kv,
+               hb_pool* pool, float* out_logits, float* out_emb, void* stream);
+
+}  // namespace
+
+extern "C" {
+
 int hb_mixed_step(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, hb_kv* kv, hb_pool* pool,
                   float* out_logits, float* out_emb, void* stream) {
   return hb_mixed_step_lora(c, d, w, nullptr, kv, pool, out_logits, out_emb, stream);
@@ -688,7 +730,32 @@ int hb_mixed_step(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, hb_kv*
 
 int hb_mixed_step_lora(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, const hb_lora* lora, hb_kv* kv,
                        hb_pool* pool, float* out_logits, float* out_emb, void* stream) {
-  if (!c || !d || !w || !kv || !w->layers || !w->tok_emb || !w->final_norm) return HB_ERR_BAD_ARG;
+  if (!w || !w->layers) return HB_ERR_BAD_ARG;
+  return mixed_step(c, d, w, lora, nullptr, kv, pool, out_logits, out_emb, stream);
+}
+
+int hb_mixed_step8(hb_ctx* c, const hb_batch_desc* d, const hb_weights8* w, hb_kv* kv, hb_pool* pool, float* out_logits,
+                   float* out_emb, void* stream) {
+  if (!c || !w || !w->layers || !kv || !kv->e4m3) return HB_ERR_BAD_ARG;
+  for (int l = 0; l < c->cfg.n_layers; ++l) {
+    const hb_layer_weights8& x = w->layers[l];
+    if (!x.attn_norm || !x.ffn_norm || !x.wqkv || !x.wo || !x.w_gate_up || !x.w_down || !x.wqkv_scale || !x.wo_scale || !x.gate_up_scale || !x.down_scale)
+      return HB_ERR_BAD_ARG;
+    if (misaligned(x.attn_norm, 8) || misaligned(x.ffn_norm, 8) || misaligned(x.wqkv, 16) || misaligned(x.wo, 16) || misaligned(x.w_gate_up, 16) ||
+        misaligned(x.w_down, 16) || misaligned(x.wqkv_scale, 4) || misaligned(x.wo_scale, 4) || misaligned(x.gate_up_scale, 4) || misaligned(x.down_scale, 4))
+      return HB_ERR_BAD_ARG;
+  }
+  const hb_weights rest = {w->tok_emb, nullptr, w->final_norm, w->lm_head};
+  return mixed_step(c, d, &rest, nullptr, w->layers, kv, pool, out_logits, out_emb, stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+int mixed_step(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, const hb_lora* lora, const hb_layer_weights8* layers8, hb_kv* kv,
+               hb_pool* pool, float* out_logits, float* out_emb, void* stream) {
+  if (!c || !d || !w || !kv || !w->tok_emb || !w->final_norm) return HB_ERR_BAD_ARG;
   if (lora && (lora->rank < 1 || lora->rank > HB_LORA_MAX_RANK || !lora->layers || !(lora->scale == lora->scale)))
     return HB_ERR_BAD_ARG;
   if (!kv->arena || (!kv->has_map && !kv->e4m3)) return HB_ERR_BAD_ARG;
@@ -942,7 +1009,30 @@ int hb_mixed_step_lora(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, c
     c->pdl = pdl_enabled;             \
   } while (0)
 
-  for (int l = 0; l < cfg.n_layers; ++l) {
+  // append and attention of layer l over an 8-bit cache, from the fp16 QKV rows in act
+  auto attend8 = [&](int l) -> int {
+    r8.arena = static_cast<uint8_t*>(kv->arena) + l * r8.page_stride * kv->n_pages;
+    HB_TRY(HB_CLASS_NORM_ROPE, hb_launch_kv8_append(c, r8, ap8, s, c->pdl));
+    int n_attn = 0;
+    HB_TRY(HB_CLASS_ATTENTION, hb_launch_kv8_attention(c, r8, c->q, n_q, c->attn_out, n_q, 1.0f / sqrtf(static_cast<float>(cfg.head_dim)),
+                                                       ex->lay.kv8_split_keys, c->act, s, c->pdl, &n_attn));
+    launches += n_attn - 1;
+    return HB_OK;
+  };
+  for (int l = 0; layers8 && l < cfg.n_layers; ++l) {
+    const Layer8 y{c, layers8[l], T, s};
+    if (l == 0) HB_TRY(HB_CLASS_NORM_ROPE, hb_launch_embed_norm(c, w->tok_emb, y.w.attn_norm, s));   // (its fp16 rows are not used)
+    HB_TRY(HB_CLASS_NORM_ROPE, y.norm(y.w.attn_norm));
+    HB_TRY(HB_CLASS_GEMM, y.project(c->h, cfg.d_model, y.w.wqkv, y.w.wqkv_scale, c->act, n_qkv, cfg.d_model, HB_DTYPE_F16, false, false));
+    if ((rc = attend8(l)) != HB_OK) return rc;
+    HB_TRY(HB_CLASS_NORM_ROPE, y.codes(c->attn_out, n_q));
+    HB_TRY(HB_CLASS_GEMM, y.project(c->attn_out, 2 * n_q, y.w.wo, y.w.wo_scale, c->x, cfg.d_model, n_q, HB_DTYPE_F32, true, false));
+    HB_TRY(HB_CLASS_NORM_ROPE, y.norm(y.w.ffn_norm));
+    HB_TRY(HB_CLASS_GEMM, y.project(c->h, cfg.d_model, y.w.w_gate_up, y.w.gate_up_scale, c->act, 2 * cfg.d_ffn, cfg.d_model, HB_DTYPE_F16, false, true));
+    HB_TRY(HB_CLASS_NORM_ROPE, y.codes(c->act, cfg.d_ffn));
+    HB_TRY(HB_CLASS_GEMM, y.project(c->act, 2 * cfg.d_ffn, y.w.w_down, y.w.down_scale, c->x, cfg.d_model, cfg.d_ffn, HB_DTYPE_F32, true, false));
+  }
+  for (int l = 0; !layers8 && l < cfg.n_layers; ++l) {
     const hb_layer_weights& lw = w->layers[l];
     if (!lw.attn_norm || !lw.wqkv || !lw.wo || !lw.ffn_norm || !lw.w_gate_up || !lw.w_down) return HB_ERR_BAD_ARG;
     if (misaligned(lw.attn_norm, 8) || misaligned(lw.ffn_norm, 8)) return HB_ERR_BAD_ARG;
@@ -1021,12 +1111,7 @@ int hb_mixed_step_lora(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, c
       ga.C = c->act;
       HB_TRY(HB_CLASS_GEMM, hb_gemm_launch(c->tm_h, wm.qkv, v_qkv, HB_EPI_F16, ga, c->num_sms, s,
                                            use_lora ? &c->tm_lora_u : nullptr, use_lora ? &lm->b_qkv : nullptr, c->pdl));
-      r8.arena = static_cast<uint8_t*>(kv->arena) + l * r8.page_stride * kv->n_pages;
-      HB_TRY(HB_CLASS_NORM_ROPE, hb_launch_kv8_append(c, r8, ap8, s, c->pdl));
-      int n_attn = 0;
-      HB_TRY(HB_CLASS_ATTENTION, hb_launch_kv8_attention(c, r8, c->q, n_q, c->attn_out, n_q, 1.0f / sqrtf(static_cast<float>(cfg.head_dim)),
-                                                         ex->lay.kv8_split_keys, c->act, s, c->pdl, &n_attn));
-      launches += n_attn - 1;
+      if ((rc = attend8(l)) != HB_OK) return rc;
     } else {
       HB_TRY(HB_CLASS_GEMM, hb_gemm_launch(c->tm_h, wm.qkv, v_qkv, HB_EPI_QKV_ROPE, ga, c->num_sms, s,
                                            use_lora ? &c->tm_lora_u : nullptr, use_lora ? &lm->b_qkv : nullptr, c->pdl));
@@ -1096,6 +1181,10 @@ int hb_mixed_step_lora(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, c
   c->pdl = false;
   return HB_OK;
 }
+
+}  // namespace
+
+extern "C" {
 
 int hb_argmax(hb_ctx* c, const float* logits, int32_t n_rows, int32_t* out_tokens, void* stream) {
   if (!c || n_rows < 0 || (n_rows > 0 && (!logits || !out_tokens))) return HB_ERR_BAD_ARG;

@@ -72,7 +72,10 @@ def build_batch(entries, page_size):
 class Engine:
     def __init__(self, shape, weights, n_pages, n_slots, max_tokens, max_segs, max_pos,
                  kv_fill=None, pool_fill=None, device="cuda", lora=None, kv_dtype="f16"):
-        """kv_dtype: "f16", or "e4m3" for the 8-bit cache (half the memory per token)."""
+        """kv_dtype: "f16", or "e4m3" for the 8-bit cache (half the memory per token).  weights: binding.DeviceWeights, or
+        binding.DeviceWeights8 for 8-bit projections (over the 8-bit cache, without adapters)."""
+        if isinstance(weights, B.DeviceWeights8) and (kv_dtype != "e4m3" or lora is not None):
+            raise ValueError("8-bit weights need kv_dtype='e4m3' and no adapters")
         if kv_dtype not in ("f16", "e4m3"):
             raise ValueError(f"kv_dtype: 'f16' or 'e4m3', not {kv_dtype!r}")
         self.shape = shape
