@@ -21,6 +21,8 @@
 #include <cuda_fp8.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "hb_internal.h"
 #include "ptx.cuh"
 
@@ -88,7 +90,9 @@ __device__ __forceinline__ void activate(float (&z)[SIZE], int act) {
 // allows.  The residual comes in the same way, into the same place, ahead of the sums.
 struct Block {
   const LinArgs& a;
-  uint32_t buf;         // shared memory of this block
+  char* mem;            // this block in shared memory, and its address there
+  uint32_t buf;
+  bool issuer;          // the thread that issues the warp's copies, and waits for them
   int lane, row0, tokens, col0;   // first row and how many are this group's; first output column
 
   __device__ __forceinline__ int width() const { return a.l.gated ? 16 : 32; }
@@ -97,35 +101,10 @@ struct Block {
   __device__ __forceinline__ bool whole() const { return tokens == 32 || row0 + tokens == a.l.m; }   // no row of another group
 
   template <int V>
-  static __device__ __forceinline__ void copy_out(char* g, uint32_t s) {
-    if constexpr (V == 16) {
-      uint4 q;
-      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(s));
-      *reinterpret_cast<uint4*>(g) = q;
-    } else if constexpr (V == 8) {
-      uint2 q;
-      asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(q.x), "=r"(q.y) : "r"(s));
-      *reinterpret_cast<uint2*>(g) = q;
-    } else if constexpr (V == 4) {
-      uint32_t q;
-      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(q) : "r"(s));
-      *reinterpret_cast<uint32_t*>(g) = q;
-    } else {
-      unsigned short q;
-      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(q) : "r"(s));
-      *reinterpret_cast<unsigned short*>(g) = q;
-    }
-  }
-  template <int V>
-  static __device__ __forceinline__ void copy_in(const char* g, uint32_t s) {
-    if constexpr (V == 16) {
-      cp_async16(s, g, true);
-    } else if constexpr (V >= 4) {
-      cp_async_small<V>(s, g, true);
-    } else {
-      const unsigned short q = *reinterpret_cast<const unsigned short*>(g);
-      asm volatile("st.shared.u16 [%0], %1;" ::"r"(s), "h"(q) : "memory");
-    }
+  static __device__ __forceinline__ void copy_in(const char* g, uint32_t s, char* m) {
+    if constexpr (V == 16) cp_async16(s, g, true);
+    else if constexpr (V >= 4) cp_async_small<V>(s, g, true);
+    else *reinterpret_cast<unsigned short*>(m) = *reinterpret_cast<const unsigned short*>(g);
   }
   // the block's rows, V bytes per lane and access, between shared memory and `base`
   template <int V, bool OUT>
@@ -134,12 +113,13 @@ struct Block {
     const int token = lane >> shift, at = (lane - (token << shift)) * V, step = 32 >> shift;   // first token, byte in its row, tokens per pass
     if (at >= cols() * size) return;        // (V divides the row's bytes)
     char* g = base + (row0 + token) * stride_bytes + col0 * size + at;
-    uint32_t s = buf + lane * V;
+    using Vec = typename std::conditional<V == 16, uint4, typename std::conditional<V == 8, uint2, typename std::conditional<V == 4, uint32_t, unsigned short>::type>::type>::type;
+    int s = lane * V;
     stride_bytes *= step;
 #pragma unroll 8
     for (int i = token; i < tokens; i += step, g += stride_bytes, s += 32 * V) {
-      if constexpr (OUT) copy_out<V>(g, s);
-      else copy_in<V>(g, s);
+      if constexpr (OUT) *reinterpret_cast<Vec*>(g) = *reinterpret_cast<const Vec*>(mem + s);
+      else copy_in<V>(g, buf + s, mem + s);
     }
   }
   template <bool OUT>
@@ -157,7 +137,7 @@ struct Block {
     if (a.res_tma) {
       fence_async_smem();      // what the lanes did to the buffer comes before the copy
       __syncwarp();
-      if (lane == 0) {
+      if (issuer) {
         mbar_arrive_expect_tx(bar, 32 * width() * (a.l.residual_dtype == HB_DTYPE_F32 ? 4 : 2));
         tma_load_2d(buf, map, bar, col0, row0);
       }
@@ -167,25 +147,20 @@ struct Block {
     }
   }
   // element e of a lane is token e, or 2 e + (lane & 1) where pairs of lanes became one column (NE = 16)
-  template <int NE>
-  __device__ __forceinline__ uint32_t place(int e, int size) const {
-    return buf + (NE == 32 ? e * 32 + lane : (2 * e + (lane & 1)) * 16 + (lane >> 1)) * size;
+  template <int NE, typename T>
+  __device__ __forceinline__ T* place(int e) const {
+    return reinterpret_cast<T*>(mem) + (NE == 32 ? e * 32 + lane : (2 * e + (lane & 1)) * 16 + (lane >> 1));
   }
   template <int NE>
   __device__ __forceinline__ void add_residual(float (&z)[32]) const {
     if (a.l.residual_dtype == HB_DTYPE_F32) {
 #pragma unroll
-      for (int e = 0; e < NE; ++e) {
-        float v;
-        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(place<NE>(e, 4)));
-        z[e] += v;
-      }
+      for (int e = 0; e < NE; ++e) z[e] += *place<NE, float>(e);
     } else {
       const bool bf16 = a.l.residual_dtype == HB_DTYPE_BF16;
 #pragma unroll
       for (int e = 0; e < NE; ++e) {
-        unsigned short v;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(place<NE>(e, 2)));
+        const unsigned short v = *place<NE, unsigned short>(e);
         z[e] += bf16 ? __uint_as_float(static_cast<uint32_t>(v) << 16) : __half2float(__ushort_as_half(v));
       }
     }
@@ -194,14 +169,14 @@ struct Block {
   __device__ __forceinline__ void lay_down(const float (&z)[32]) const {
     if (a.l.c_dtype == HB_DTYPE_F32) {
 #pragma unroll
-      for (int e = 0; e < NE; ++e) asm volatile("st.shared.f32 [%0], %1;" ::"r"(place<NE>(e, 4)), "f"(z[e]) : "memory");
+      for (int e = 0; e < NE; ++e) *place<NE, float>(e) = z[e];
     } else {
       const bool bf16 = a.l.c_dtype == HB_DTYPE_BF16;
 #pragma unroll
       for (int e = 0; e < NE; e += 2) {
         const uint32_t w = bf16 ? pack_bf16x2(z[e], z[e + 1]) : pack_f16x2_satfinite(z[e], z[e + 1]);
-        asm volatile("st.shared.u16 [%0], %1;" ::"r"(place<NE>(e, 2)), "h"(static_cast<unsigned short>(w)) : "memory");
-        asm volatile("st.shared.u16 [%0], %1;" ::"r"(place<NE>(e + 1, 2)), "h"(static_cast<unsigned short>(w >> 16)) : "memory");
+        *place<NE, unsigned short>(e) = static_cast<unsigned short>(w);
+        *place<NE, unsigned short>(e + 1) = static_cast<unsigned short>(w >> 16);
       }
     }
   }
@@ -263,13 +238,13 @@ struct Block {
     if (a.c_tma && whole()) {
       fence_async_smem();
       __syncwarp();
-      if (lane == 0) tma_store_2d(map, buf, col0, row0);
+      if (issuer) tma_store_2d(map, buf, col0, row0);
     } else {
       __syncwarp();
       copy<true>(a.l.c, a.l.c_stride, a.l.c_dtype, a.c_vec);
       __syncwarp();
     }
-    if (lane == 0) tma_store_commit();   // one group per block, empty or not: waits count them
+    if (issuer) tma_store_commit();   // one group per block, empty or not: waits count them
   }
 };
 
@@ -319,22 +294,27 @@ struct Tile {
 };
 template <int BT>
 __device__ __forceinline__ Tile tile_of(const LinArgs& a, const int* lo, const int* hi, const int* pre, int item) {
-  const int q = item / a.f_tiles;
-  int b = 0, e = a.n_groups;     // last group whose first tile is <= q
-  while (e - b > 1) {
-    const int mid = (b + e) >> 1;
-    if (pre[mid] <= q) b = mid; else e = mid;
+  int b = 0;
+  if (a.n_groups > 1) {
+    const int q = item / a.f_tiles;
+    int e = a.n_groups;            // last group whose first tile is <= q
+    while (e - b > 1) {
+      const int mid = (b + e) >> 1;
+      if (pre[mid] <= q) b = mid; else e = mid;
+    }
   }
   const int tiles = pre[b + 1] - pre[b];
-  const int local = item - pre[b] * a.f_tiles;
-  // features over bands of token tiles, tokens fastest inside a band
-  const int per_band = a.band * a.f_tiles;
-  const int band = local / per_band, in_band = local - band * per_band;
-  const int height = min(a.band, tiles - band * a.band);
+  int local = item - pre[b] * a.f_tiles, first = 0, height = tiles;
+  if (a.band < tiles) {            // features over bands of token tiles, tokens fastest inside a band
+    const int per_band = a.band * a.f_tiles, band = local / per_band;
+    local -= band * per_band;
+    first = band * a.band;
+    height = min(a.band, tiles - first);
+  }
   Tile t;
   t.group = b;
-  t.feature_tile = in_band / height;
-  t.row0 = lo[b] + (band * a.band + in_band - t.feature_tile * height) * BT;
+  t.feature_tile = local / height;
+  t.row0 = lo[b] + (first + local - t.feature_tile * height) * BT;
   t.rows = min(BT, hi[b] - t.row0);
   return t;
 }
@@ -394,14 +374,20 @@ __device__ __forceinline__ void issue_block(uint32_t d, uint64_t wdesc, uint64_t
   }
 }
 
-template <int CG, int BT, bool LONG>
+// How a persistent CTA's epilogue works.  PLAIN: 8 warps, a residual ahead.  LONG: tensor memory holds a tile's sums for SEG_BLOCKS k-blocks
+// at a time, and registers (of 16 warps) add them up.  The tensor cores cut what falls off the end of a sum, 2^-26 of it per
+// instruction on average and always towards zero (fp16, K = 14336: 1.7e-5 in all); additions in registers round.  For fp32
+// outputs; with 16 bits out the loss is far below the rounding.  SHORT: 16 warps, for products of so few k-blocks that the
+// results bound them (4096 x 4096 x 64 fp16: 17.9 us, with 8 warps 19.8; at K = 4096 the 8 warps' larger ring wins by 2 %).
+enum { PLAIN = 0, LONG = 1, SHORT = 2 };
+
+template <int CG, int BT, int MODE>
 struct Shape {
   static constexpr int TOKENS = BT / CG;                        // token rows a CTA holds per stage
   static constexpr int BOX = TOKENS < 64 ? TOKENS : 64;         // token rows per copy
   static constexpr int W_BYTES = BF * BKB;
-  // epilogue warps: four per 32 tokens of the tile, up to 8 (16 where they hold sums in registers); a warp has BT / 32 / PARTS
-  // blocks of 32 tokens
-  static constexpr int MOST = LONG ? 16 : 8;
+  // epilogue warps: four per 32 tokens of the tile, up to 8 or 16; a warp has BT / 32 / PARTS blocks of 32 tokens
+  static constexpr int MOST = MODE == PLAIN ? 8 : 16;
   static constexpr int EPI_WARPS = BT / 8 < MOST ? BT / 8 : MOST;
   static constexpr int PARTS = EPI_WARPS / 4;
   static constexpr int THREADS = 64 + EPI_WARPS * 32;
@@ -427,14 +413,11 @@ __device__ __forceinline__ void read_sums(uint32_t at, float (&z)[32]) {
 }
 
 // SPLIT: the CTAs of a cluster share one tile's K range (CG = 1), two CTAs per SM; otherwise one persistent CTA per SM.
-// LONG: tensor memory holds a tile's sums for SEG_BLOCKS k-blocks at a time, and registers add them up.  The tensor cores cut
-// what falls off the end of a sum, 2^-26 of it per instruction on average and always towards zero (fp16, K = 14336: 1.7e-5 in all);
-// additions in registers round.  For fp32 outputs; with 16 bits out the loss is far below the rounding.
-template <int CG, int BT, bool SPLIT, bool LONG>
-__global__ void __launch_bounds__(Shape<CG, BT, LONG>::THREADS, SPLIT ? 2 : 1)
+template <int CG, int BT, bool SPLIT, int MODE>
+__global__ void __launch_bounds__(Shape<CG, BT, MODE>::THREADS, SPLIT ? 2 : 1)
 linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_c,
               const __grid_constant__ CUtensorMap tm_res, const LinArgs a) {
-  using S = Shape<CG, BT, LONG>;
+  using S = Shape<CG, BT, MODE>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -567,8 +550,8 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
       for (int item = worker; ok && item < total; item += n_workers) {
         const int rows = __shfl_sync(0xffffffffu, tile_of<BT>(a, g_lo, g_hi, g_pre, item).rows, 0);
         const uint32_t idesc = make_idesc_f16(BF * CG, mma_n(rows), false) | format;
-        for (int seg0 = kb0; ok && seg0 < kb1; seg0 += LONG ? SEG_BLOCKS : kb1 - kb0) {
-          const int seg1 = LONG ? min(seg0 + SEG_BLOCKS, kb1) : kb1;
+        for (int seg0 = kb0; ok && seg0 < kb1; seg0 += MODE == LONG ? SEG_BLOCKS : kb1 - kb0) {
+          const int seg1 = MODE == LONG ? min(seg0 + SEG_BLOCKS, kb1) : kb1;
           ok = __all_sync(0xffffffffu, mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag, WAIT_LIMIT_NS));
           if (!ok) { give_up(); break; }
           tc_fence_after();
@@ -609,6 +592,8 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
     const int part = (warp - 2) >> 2;        // which blocks of 32 tokens
     const int ew = warp - 2;
     const uint32_t bufs = smem_base + stage_bytes + ew * a.bufs * a.buf_bytes;
+    char* buf_mem = reinterpret_cast<char*>(smem_gen + stage_bytes + ew * a.bufs * a.buf_bytes);
+    const bool issuer = elect_one();
     float* scales = reinterpret_cast<float*>(smem_gen + stage_bytes + S::EPI_WARPS * a.bufs * a.buf_bytes) + ew * 32;
     uint32_t buf_phase = 0;                  // a bit per buffer: parity of its next residual
     int buf = 0;
@@ -642,14 +627,14 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
       const int64_t f_at = static_cast<int64_t>(t.group) * a.l.n + f0 + lane;
       const float factor = mine && a.l.w_scale ? a.l.w_scale[f_at] : 1.0f, bias = mine && a.l.bias ? a.l.bias[f_at] : 0.0f;
       auto block_at = [&](const Tile& tile, int feature, int c, int i) {
-        return Block{a, bufs + static_cast<uint32_t>(i * a.buf_bytes), lane, tile.row0 + c, min(32, tile.rows - c), a.l.gated ? feature >> 1 : feature};
+        return Block{a, buf_mem + i * a.buf_bytes, bufs + static_cast<uint32_t>(i * a.buf_bytes), issuer, lane, tile.row0 + c, min(32, tile.rows - c), a.l.gated ? feature >> 1 : feature};
       };
       auto block_of = [&](int c, int i) { return block_at(t, f0, c, i); };
       // buffer i can be written: what was copied out of it has been read
       auto free_buffer = [&]() {
-        if (lane == 0) {
-          if constexpr (LONG) tma_store_wait_read<0>();
-          else tma_store_wait_read<1>();     // (two buffers, or three where the next residual goes into one meanwhile)
+        if (issuer) {
+          if (MODE == PLAIN) tma_store_wait_read<1>();   // (two buffers, or three where the next residual goes into one meanwhile)
+          else tma_store_wait_read<0>();                 // (one, or two)
         }
         __syncwarp();
       };
@@ -672,7 +657,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
       auto column = [&](int acc_i, int c) {
         return tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(acc_i * BT + c);
       };
-      if constexpr (LONG) {
+      if constexpr (MODE == LONG) {
         constexpr int PIECES = BT / 32 / S::PARTS;
         float z[PIECES][32];
 #pragma unroll
@@ -743,7 +728,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
         if (!ok) { give_up(); break; }
       }
     }
-    if (lane == 0) tma_store_wait_all();     // shared memory stays until it has been read
+    if (issuer) tma_store_wait_all();        // shared memory stays until it has been read
   } else if (worker < total) {
     mbar_wait(tfull_bar(0), 0u, abort_flag, WAIT_LIMIT_NS);
     __syncwarp();
@@ -993,9 +978,9 @@ int row_vector(const void* p, int64_t stride, int size, int cols) {
   return v;
 }
 
-template <int CG, int BT, bool SPLIT, bool LONG>
+template <int CG, int BT, bool SPLIT, int MODE>
 int launch_as(const hb_linear_args& l, LinArgs a, int splits, int num_sms, int64_t w_group_stride, cudaStream_t s, bool pdl) {
-  using S = Shape<CG, BT, LONG>;
+  using S = Shape<CG, BT, MODE>;
   const int ab = elem_bytes(l.ab_dtype);
   CUtensorMap tw, ta;
   const uint64_t k_bytes = static_cast<uint64_t>(l.k) * ab;
@@ -1023,7 +1008,7 @@ int launch_as(const hb_linear_args& l, LinArgs a, int splits, int num_sms, int64
       if (a.res_tma && (rc = hb_tmap_block(&tr, l.residual, l.residual_dtype, cols, l.m, l.residual_stride * rs, width, 32)) != HB_OK) return rc;
     }
   }
-  a.bufs = LONG ? 1 : l.residual ? 3 : 2;
+  a.bufs = (MODE == PLAIN ? 2 : 1) + (MODE != LONG && l.residual ? 1 : 0);
   a.buf_bytes = 32 * width * (cs > rs ? cs : rs);
   const int fixed = 1024 + S::BAR_BYTES + (SPLIT ? 0 : S::EPI_WARPS * a.bufs * a.buf_bytes + S::SCALE_BYTES) + table;
   const int room = (SPLIT ? 113 : 227) * 1024;
@@ -1031,7 +1016,7 @@ int launch_as(const hb_linear_args& l, LinArgs a, int splits, int num_sms, int64
   if (a.stages > MAX_STAGES) a.stages = MAX_STAGES;
   const int smem = fixed + a.stages * S::STAGE_BYTES;
   static DynSmemState configured;
-  auto kern = linear_kernel<CG, BT, SPLIT, LONG>;
+  auto kern = linear_kernel<CG, BT, SPLIT, MODE>;
   if (hb_ensure_dyn_smem(reinterpret_cast<const void*>(kern), configured, smem) != HB_OK) return HB_ERR_CUDA;
   int64_t workers = items;
   if (!SPLIT && workers > num_sms / CG) workers = num_sms / CG;
@@ -1073,9 +1058,12 @@ template <int CG, int BT, bool SPLIT>
 int launch(const hb_linear_args& l, const LinArgs& a, int splits, int num_sms, int64_t w_group_stride, cudaStream_t s, bool pdl) {
   if constexpr (!SPLIT) {
     if (l.c_dtype == HB_DTYPE_F32 && a.k_blocks > SEG_BLOCKS)
-      return launch_as<CG, BT, SPLIT, true>(l, a, splits, num_sms, w_group_stride, s, pdl);
+      return launch_as<CG, BT, SPLIT, LONG>(l, a, splits, num_sms, w_group_stride, s, pdl);
+    if constexpr (BT >= 128) {
+      if (a.k_blocks <= (BT == 128 ? 8 : 12)) return launch_as<CG, BT, SPLIT, SHORT>(l, a, splits, num_sms, w_group_stride, s, pdl);
+    }
   }
-  return launch_as<CG, BT, SPLIT, false>(l, a, splits, num_sms, w_group_stride, s, pdl);
+  return launch_as<CG, BT, SPLIT, PLAIN>(l, a, splits, num_sms, w_group_stride, s, pdl);
 }
 
 // Which kernel: tokens of a tile (8, 16: linear_narrow_kernel; 32 .. 128: one CTA per tile; 256: a pair), and `share`: 16-feature
@@ -1123,7 +1111,7 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
     if (bt < 128 && rows > 4 * bt) continue;
     const float features = ceil_div(l.n, bt == 256 ? 2 * BF : BF), tiles = features * token_tiles(bt);
     const float block_us = bt <= 64 ? 0.205f : bt == 128 ? (f8 ? 0.25f : 0.22f) : 0.28f;   // a k-block's products
-    const float out_us = bt == 32 ? 0.7f : bt == 64 ? 1.0f : bt == 128 ? 2.0f : 4.0f;      // a tile's epilogue
+    const float out_us = bt == 32 ? 0.9f : bt == 64 ? 1.25f : bt == 128 ? 2.0f : 4.0f;      // a tile's epilogue
     const float main_us = k_blocks * block_us, waves = ceil_div(tiles, bt == 256 ? sms / 2 : sms);
     const float us = 4.2f + main_us + out_us + (waves - 1.0f) * (main_us > out_us ? main_us : out_us);
     offer(bt, 1, us > weight_us + 4.5f ? us : weight_us + 4.5f);
