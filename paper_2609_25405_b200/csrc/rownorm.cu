@@ -28,6 +28,7 @@ struct RowArgs {
   int32_t n_rows, n_src, d;
   int32_t x_bf16, res_bf16, y_dtype;
   int32_t lead0, lead_step;   // elements between a 16-byte boundary and the start of row r: (lead0 + r lead_step) mod 8
+  int32_t turned, y_lead0, y_lead_step;   // hb_quant_rows: codes not aligned as x is go through `turned` bytes of shared memory per row
   float eps;
 };
 
@@ -130,7 +131,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
     }
     src = i;
   }
-  const int lead = E == 8 ? static_cast<int>((a.lead0 + r * a.lead_step) & 7) : 0;
+  const int lead = E == 8 ? static_cast<int>((a.lead0 + src * a.lead_step) & 7) : 0;
   const char* x = static_cast<const char*>(a.x) + src * a.x_stride * XB;
   const char* res = RB ? static_cast<const char*>(a.res) + r * a.res_stride * RB : nullptr;
   auto first = [&](int i) { return (tid + i * T) * E - lead; };
@@ -214,6 +215,34 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
     inv = finite ? 448.0f / m : __int_as_float(0x7fffffff);
     if (tid == 0) a.scale[r] = finite ? m / 448.0f : __int_as_float(0x7fffffff);
   }
+  if constexpr (!NORM && E == 8) {
+    if (a.turned) {
+      // codes where the boundaries of their own row lie, then out in 8-byte accesses
+      extern __shared__ unsigned char codes[];
+      const int y_lead = static_cast<int>((a.y_lead0 + r * a.y_lead_step) & 7);
+      unsigned char* mine = codes + threadIdx.x / T * a.turned;
+      unsigned char* y = static_cast<unsigned char*>(a.y) + r * a.y_stride;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int at = first(i);
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+          if (at + j >= 0 && at + j < a.d) mine[y_lead + at + j] = __nv_cvt_float_to_fp8(rx[i].get(j, a.x_bf16) * inv, __NV_SATFINITE, __NV_E4M3);
+      }
+      if constexpr (T == 32) __syncwarp();
+      else __syncthreads();
+      for (int i = tid * 8; i < y_lead + a.d; i += T * 8) {
+        const int at = i - y_lead;
+        if (whole(at)) {
+          *reinterpret_cast<uint2*>(y + at) = *reinterpret_cast<const uint2*>(mine + i);
+        } else {
+          for (int j = 0; j < 8; ++j)
+            if (at + j >= 0 && at + j < a.d) y[at + j] = mine[i + j];
+        }
+      }
+      return;
+    }
+  }
   char* y = static_cast<char*>(a.y) + r * a.y_stride * (a.y_dtype == HB_DTYPE_E4M3 ? 1 : a.y_dtype == HB_DTYPE_F32 ? 4 : 2);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -237,7 +266,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
 template <int XB, int RB, int T, int NV, int E, bool NORM>
 int launch(const RowArgs& a, cudaStream_t s, bool pdl) {
   const unsigned grid = T == 32 ? (a.n_rows + 7) / 8 : a.n_rows;
-  return hb_launch_kernel(row_kernel<XB, RB, T, NV, E, NORM>, grid, T == 32 ? 256 : T, 0, s, pdl, a);
+  return hb_launch_kernel(row_kernel<XB, RB, T, NV, E, NORM>, grid, T == 32 ? 256 : T, (T == 32 ? 8 : 1) * a.turned, s, pdl, a);
 }
 
 // Threads of a row and vectors of a thread.  An SM needs some 40 KB under way: where a vector is few bytes (no residual), four a
@@ -246,6 +275,7 @@ int launch(const RowArgs& a, cudaStream_t s, bool pdl) {
 template <int XB, int RB, bool NORM>
 int launch_size(const RowArgs& a, bool wide, bool many, cudaStream_t s, bool pdl) {
   if (!wide) {
+    if constexpr (!NORM) return launch<XB, RB, 1024, 32, 1, NORM>(a, s, pdl);   // (only the last few lengths)
     if (a.d <= 256) return launch<XB, RB, 32, 8, 1, NORM>(a, s, pdl);
     if (a.d <= 2048) return launch<XB, RB, 256, 8, 1, NORM>(a, s, pdl);
     if (a.d <= 8192) return launch<XB, RB, 1024, 8, 1, NORM>(a, s, pdl);
@@ -268,7 +298,7 @@ int launch_size(const RowArgs& a, bool wide, bool many, cudaStream_t s, bool pdl
   if (d <= 8192) return launch<XB, RB, 512, 2, 8, NORM>(a, s, pdl);
   if (d <= 16384) return launch<XB, RB, 1024, 2, 8, NORM>(a, s, pdl);
   if (d <= 32768) return launch<XB, RB, 1024, 4, 8, NORM>(a, s, pdl);
-  return launch<XB, RB, 1024, 32, 1, NORM>(a, s, pdl);
+  return launch<XB, RB, 1024, 32, 1, NORM>(a, s, pdl);   // (the last few lengths, off a boundary)
 }
 
 // The rows of one array: first element, elements between rows, bytes of an element.
@@ -335,7 +365,14 @@ int hb_launch_quant_rows(hb_ctx* c, const void* x, int x_dtype, int64_t x_stride
   a.n_rows = n_rows; a.n_src = n_src; a.d = d;
   a.x_bf16 = x_dtype == HB_DTYPE_BF16; a.y_dtype = HB_DTYPE_E4M3;
   const int xb = elem_bytes(x_dtype);
-  const bool wide = aligned_alike({{x, x_stride, xb}, {codes, codes_stride, 1}}, &a) && (!index || a.lead_step == 0);   // (an index breaks the step)
+  if (!aligned_alike({{x, x_stride, xb}, {codes, codes_stride, 1}}, &a) || (index && a.lead_step)) {   // (an index breaks the step)
+    a.y_lead0 = static_cast<int32_t>(reinterpret_cast<uintptr_t>(codes) % 8);
+    a.y_lead_step = static_cast<int32_t>(codes_stride % 8);
+    a.turned = (d + 7 + 15) / 16 * 16;
+    aligned_alike({{x, x_stride, xb}}, &a);
+  }
+  const bool wide = ((a.lead0 | a.lead_step) & 7) == 0 || d + 7 <= HB_NORM_MAX_D;
+  if (!wide) a.turned = 0;
   const bool many = n_rows >= 2 * c->num_sms;
   return xb == 4 ? launch_size<4, 0, false>(a, wide, many, s, pdl) : launch_size<2, 0, false>(a, wide, many, s, pdl);
 }

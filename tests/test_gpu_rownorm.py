@@ -142,6 +142,23 @@ def test_quant_rows(rows, d, x_t):
     assert torch.equal(c2.float(), codes[index.long()].float()) and torch.equal(s2, scale[index.long()])
 
 
+@pytest.mark.parametrize("x_t", [F32, F16])
+@pytest.mark.parametrize("d", [5, 61, 1000, 1001, 4095, 14335, 32760, 32765, 32767])
+def test_quant_of_rows_off_every_boundary(d, x_t):
+    """Source rows and codes at offsets and strides that have nothing in common; nothing beside the rows is written."""
+    g = gen(d)
+    for x_pitch, x_off, c_pitch, c_off in ((d + 3, 1, d + 5, 2), (d + 8, 0, d + 1, 1), (d + 1, 1, d + 16, 3)):
+        x, _ = strided(7, d, x_t, x_pitch, x_off)
+        x.copy_(torch.randn(7, d, generator=g, device="cuda"))
+        c, whole = strided(5, d, E4M3, c_pitch, c_off, fill=3.0)
+        index = torch.tensor([6, 0, 3, 3, 1], dtype=torch.int32, device="cuda")
+        scale = torch.empty(5, device="cuda")
+        ctx().quant_rows(x, c, scale, index=index)
+        _check_rows(c, x.double()[index.long()], scale)
+        c.copy_(torch.full((5, d), 3.0, device="cuda").to(E4M3))
+        assert bool((whole.float() == 3.0).all())
+
+
 @pytest.mark.parametrize("d", [96, 2048, 6001])
 def test_quant_index_that_names_no_row(d):
     """Negative: the row stays; beyond the source: the row stays and the call is reported."""
