@@ -7,14 +7,21 @@
 // what it holds.  Operands are moved and multiplied as bytes: a k-block is 128 bytes of K (64 elements of 16
 // bits, 128 of 8), a row of the 128-byte swizzle, and four instructions of 32 bytes each; only the instruction's kind differs.
 //
-//   warp 0     TMA: the tile's weight rows and token rows of one k-block per stage
-//   warp 1     one thread issues the MMAs; accumulators in tensor memory, two of them where a CTA walks several tiles
-//   warps 2-9  epilogue: a warp reads 32 features x 32 tokens, turns them through shared memory, and finishes four adjacent
-//              features of a token per thread
+//   warp 0   TMA: the tile's weight rows and token rows of one k-block per stage
+//   warp 1   issues the MMAs; two accumulators in tensor memory where a CTA walks several tiles.  The whole warp walks the stages
+//            and one elected thread issues: with one thread walking, the compiler has to prove the instructions' operands
+//            uniform one by one, and a k-block of one CTA took 0.43 us instead of 0.20 (the 4096 x 28672 x 4096 case 435 -> 357 us).
+//   others   epilogue: a warp takes 32 features x 32 tokens, a feature per lane, applies scales, bias and activation, adds the
+//            residual that a TMA copy brought meanwhile, and sends the block out by another
 //
 //   CG = 2     a pair of CTAs per 256 x 256 tile (cta_group::2), persistent: many tokens
-//   CG = 1     one CTA per 128 x BT tile; persistent, or a cluster of S CTAs that share the tile's K range (few tiles): each
-//              computes its share, hands the partial sums of the tokens of rank r to CTA r, which adds them in rank order
+//   CG = 1     one CTA per 128 x BT tile; persistent, or a cluster of four or eight CTAs that share the tile's K range (few tiles):
+//              each computes its share, hands the partial sums of the tokens of rank r to CTA r, which adds them in rank order
+//   few rows   linear_narrow_kernel below
+//
+// What bounds it (one B200, 148 SMs): 4096 x 28672 x 4096 e4m3 with SwiGLU 310 - 330 us, 2.9 - 3.1 PFLOP/s, the tensor pipe and the
+// power limit (a k-block takes 512 cycles of it); 64 rows of 28672 x 4096 e4m3 25 us and eight such weights 150 us, HBM
+// (4.7 and 6.2 TB/s); 2048^3 fp16 onto fp32 26 us, one wave of tiles: filling, 32 k-blocks, and an epilogue that nothing hides.
 //
 // Groups: every CTA reads the bounds, drops those that are no good and numbers the token tiles of the others; a weight is a
 // three-dimensional tensor map, so that a tile never sees the next group's rows.
@@ -1116,7 +1123,7 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
     const float us = 4.2f + main_us + out_us + (waves - 1.0f) * (main_us > out_us ? main_us : out_us);
     offer(bt, 1, us > weight_us + 4.5f ? us : weight_us + 4.5f);
     if (bt == 256) break;
-    for (int s = 2; s <= 8 && s <= k_blocks; s *= 2) {
+    for (int s = 4; s <= 8 && s <= k_blocks; s *= 2) {                         // (two never paid)
       const float ctas = tiles * s, held = rows < bt ? rows : static_cast<float>(bt);
       if (ctas > 2 * sms) break;                                               // all at once, two per SM, or not at all
       const float share_us = ceil_div(k_blocks, s) * (ctas > sms ? 0.45f : 0.3f);

