@@ -1121,7 +1121,7 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
     const float out_us = bt == 32 ? 0.9f : bt == 64 ? 1.25f : bt == 128 ? 2.0f : 4.0f;      // a tile's epilogue
     const float main_us = k_blocks * block_us, waves = ceil_div(tiles, bt == 256 ? sms / 2 : sms);
     const float us = 4.2f + main_us + out_us + (waves - 1.0f) * (main_us > out_us ? main_us : out_us);
-    offer(bt, 1, us > weight_us + 4.5f ? us : weight_us + 4.5f);
+    offer(bt, 1, us > weight_us + 4.5f ? us : weight_us + 4.5f + 0.1f * us);   // (both bound by the weights: the one with more to spare)
     if (bt == 256) break;
     for (int s = 4; s <= 8 && s <= k_blocks; s *= 2) {                         // (two never paid)
       const float ctas = tiles * s, held = rows < bt ? rows : static_cast<float>(bt);
