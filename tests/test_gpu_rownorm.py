@@ -92,6 +92,30 @@ def test_norm_views_in_wider_matrices(y_t):
         assert torch.equal(got[1], ref[1])
 
 
+@pytest.mark.parametrize("d", [3, 200, 2000, 8000, 8001, 20000])
+@pytest.mark.parametrize("x_t,r_t,y_t", [(F16, F32, E4M3), (F32, BF16, F16), (BF16, None, F32)])
+def test_norm_of_arrays_aligned_differently(d, x_t, r_t, y_t):
+    """Every array at an offset and stride of its own: no access of several elements fits them all."""
+    g = gen(d)
+    x, _ = strided(5, d, x_t, d + 3, 1)
+    x.copy_(torch.randn(5, d, generator=g, device="cuda"))
+    r = r_all = None
+    if r_t is not None:
+        r, r_all = strided(5, d, r_t, d + 6, 2, fill=7.0)
+        r.copy_(torch.randn(5, d, generator=g, device="cuda"))
+    y, y_all = strided(5, d, y_t, d + 8, 5, fill=7.0)
+    gain = (1 + 0.1 * torch.randn(d + 1, generator=g, device="cuda")).bfloat16()[1:]
+    scale = torch.empty(5, device="cuda") if y_t == E4M3 else None
+    _, want = _norm64(x, r, gain, 1e-5)
+    ctx().norm(x, gain, y, residual=r, sum_out=r, y_scale=scale, eps=1e-5)
+    _check_rows(y, want, scale)
+    y.copy_(torch.full((5, d), 7.0, device="cuda").to(y_t))
+    assert bool((y_all.float() == 7.0).all())
+    if r is not None:
+        r.fill_(7.0)
+        assert bool((r_all == 7.0).all())
+
+
 def test_norm_in_place():
     g = gen(8)
     x = torch.randn(33, 2048, generator=g, device="cuda").bfloat16()
