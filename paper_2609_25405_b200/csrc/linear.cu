@@ -1109,7 +1109,7 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
         const float rounds = ceil_div(k_bytes, 512.0f * (mt * nt == 1 ? 8 : mt * nt == 2 ? 4 : 2));   // of loads that wait for each other
         const float waves = ceil_div(blocks, 2 * sms);
         const float latency = rounds * (mt * nt == 1 ? 2.1f : mt * nt == 2 ? 1.7f : 1.4f), bytes = blocks * (16 * mt + 8 * nt) * k_bytes / 6e6f;
-        offer(8 * nt, mt, 1.0f + waves * 2.0f + (waves * latency > bytes ? waves * latency : bytes));
+        offer(8 * nt, mt, 1.0f + waves * (1.0f + mt) + (waves * latency > bytes ? waves * latency : bytes));
       }
   }
   const bool f8 = l.ab_dtype == HB_DTYPE_E4M3;

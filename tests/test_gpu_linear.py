@@ -226,7 +226,7 @@ def test_many_groups(groups):
 
 # (rows, n, k, operands, groups): between them they take every kernel: few rows, tiles of 32 to 128 tokens alone and shared by four and
 # eight CTAs, pairs; long sums onto fp32, short products
-KERNELS = [(9, 3333, 586, F16, 0), (1253, 16, 885, F16, 20), (18, 6240, 9444, E4M3, 0), (169, 2325, 3993, F16, 0), (863, 155, 3069, F16, 23),
+KERNELS = [(9, 3333, 586, F16, 0), (18, 2691, 539, F16, 0), (2, 2415, 526, F16, 3), (18, 2480, 72, F16, 0), (16, 6144, 2048, E4M3, 0), (5, 40, 4000, E4M3, 3), (1253, 16, 885, F16, 20), (18, 6240, 9444, E4M3, 0), (169, 2325, 3993, F16, 0), (863, 155, 3069, F16, 23),
            (2485, 151, 4260, F16, 0), (2032, 144, 4935, F16, 22), (66, 16, 1459, F16, 0), (133, 21, 1670, F16, 1), (313, 36, 1797, F16, 1),
            (1666, 1286, 799, F16, 0), (336, 956, 1610, F16, 18), (4100, 4100, 700, F16, 0), (520, 5000, 3000, E4M3, 0), (1300, 2570, 1030, BF16, 0)]
 
