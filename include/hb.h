@@ -616,8 +616,8 @@ HB_API int hb_logprobs(hb_ctx* ctx, const void* logits, int32_t dtype, int32_t n
  * feeds a product (hb_norm), rows brought to 8 bits (hb_quant_rows), and the product with scales,
  * bias, activation and residual in its epilogue, with one weight (hb_linear) or one per run of rows
  * (hb_linear_grouped).  Types are HB_DTYPE_*; strides are in elements and may exceed the row length.
- * E4M3 rows carry one fp32 scale each, max(their largest magnitude, 2^-100) / 448: code c stands for
- * c * scale.  A row that holds a NaN or an infinity has scale NaN and NaN codes.  fp16 outputs saturate at +-65504 (NaN stays NaN).  Nothing is allocated, and no call keeps
+ * E4M3 rows carry one fp32 scale each, max(their largest magnitude, 2^-100) / 448 (by the rounded
+ * reciprocal): code c stands for c * scale.  A row that holds a NaN or an infinity has scale NaN and NaN codes.  fp16 outputs saturate at +-65504 (NaN stays NaN).  Nothing is allocated, and no call keeps
  * anything for the next: calls of one context may run at the same time on different streams. */
 
 /* y = s / sqrt(mean(s^2) + eps) * gain with s = x (+ residual), one pass over the row.  Device pointers.
@@ -648,7 +648,8 @@ HB_API int hb_norm(hb_ctx* ctx, const hb_norm_args* args, void* stream);
 /* Rows to E4M3 with a scale each: row r of codes is row index[r] of x, or row r where index is NULL (then
  * n_src >= n_rows).  x [n_src, d] F32, F16 or BF16; index device int32 [n_rows]: a negative entry leaves its row as
  * it is, one >= n_src too and raises HB_STATUS_ROW_INDEX.  The same source row may be taken more than once.
- * codes [n_rows, d], scale float [n_rows].  Limits and alignment as hb_norm's. */
+ * codes [n_rows, d], scale float [n_rows]: a code is the e4m3 value nearest to the fp32 quotient x / scale.  Limits and alignment
+ * as hb_norm's.  Without an index, codes may lie in x's own rows, each at the start of its row (the strides' bytes equal). */
 HB_API int hb_quant_rows(hb_ctx* ctx, const void* x, int32_t x_dtype, int64_t x_stride, int32_t n_src, const int32_t* index,
                          int32_t n_rows, int32_t d, void* codes, int64_t codes_stride, float* scale, void* stream);
 

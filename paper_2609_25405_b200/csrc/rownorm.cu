@@ -8,7 +8,7 @@
 // come out of ONE reduction and an 8-bit output needs no second pass over the row.
 //
 // Measured (one B200; 6.46 TB/s is a copy): 4096 rows of 4096, fp16 + fp32 to fp32 and codes, 29 us = 6.4 TB/s; 4096 rows of 14336
-// fp16 to codes 32 us = 5.5 TB/s (gathered 36); rows off every boundary (4096 of 4097, fp16 + fp32 to codes) 52 us = 3.5 TB/s, with
+// fp16 to codes 35.6 us = 4.9 TB/s (gathered 38.9); rows off every boundary (4096 of 4097, fp16 + fp32 to codes) 52 us = 3.5 TB/s, with
 // one element per access 88.
 #include <cuda_fp8.h>
 
@@ -118,6 +118,37 @@ __device__ __forceinline__ void put(void* row, int64_t at, int dtype, bool whole
 // where `lead` elements lie between a 16-byte boundary and the row's start, so that rows of any length stay wide but for their
 // first and last vector.  E = 1: rows whose arrays are not aligned alike.
 // XB / RB: bytes of an element of x and of the residual (0 = none).  NORM: false for hb_quant_rows.
+// x / unit for the elements of a row, |x| <= 448 unit (1 + 2^-23): a product with the reciprocal, corrected once by its remainder
+// (Markstein 1990).  Before its own rounding the result is within 2^-46 of the quotient, so it has the quotient's e4m3 code
+// unless the quotient lies that near the middle of two floats beside a border of codes; the units for which one does
+// were all tried (2136 cases), and the codes are the same there too.  Rows of tiny values are lifted by a power of two, or the
+// remainder would fall below fp32's range.  (4096 x 14336 fp16: 35.6 us; a division per element 48, the reciprocal alone 34.0, with a
+// code in 10^5 beside the right one.)
+struct Quotient {
+  float unit, minus_recip, minus_lift;
+  __device__ __forceinline__ Quotient(float u, float largest) {
+    const float lift = largest < 9.094947017729282e-13f ? 1.152921504606846976e18f : 1.0f;   // 2^-40, 2^60
+    unit = u * lift;
+    minus_recip = -__frcp_rn(unit);
+    minus_lift = -lift;
+  }
+  // (the sign of a zero stays)
+  template <int E>
+  __device__ __forceinline__ void operator()(float (&x)[E]) const {
+    if constexpr (E == 1) {
+      const float n = x[0] * minus_lift, q = n * minus_recip;
+      x[0] = fmaf(fmaf(q, unit, n), minus_recip, q);
+    } else {
+      const uint64_t l2 = pack2(minus_lift, minus_lift), r2 = pack2(minus_recip, minus_recip), u2 = pack2(unit, unit);
+#pragma unroll
+      for (int i = 0; i < E; i += 2) {
+        const uint64_t n = mul2(pack2(x[i], x[i + 1]), l2), q = mul2(n, r2);
+        unpack2(fma2(fma2(q, u2, n), r2, q), x[i], x[i + 1]);
+      }
+    }
+  }
+};
+
 template <int XB, int RB, int T, int NV, int E, bool NORM>
 __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a) {
   grid_dep_wait();
@@ -165,8 +196,16 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
   float s[NORM ? NV : 1][E];
   float ss = 0.0f;
   uint32_t top = 0u;   // largest magnitude as bits: their order is that of the values, and NaN comes out on top
+  if constexpr (!NORM && XB == 2) {
+    uint32_t two = 0u;   // (16-bit values as they are, two at a time)
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < Raw<E, XB>::WORDS; ++j) two = max_u16x2(two, rx[i].w[j] & 0x7fff7fffu);
+    top = __float_as_uint(from16(max(two >> 16, two & 0xffffu), a.x_bf16)) & 0x7fffffffu;
+  }
+#pragma unroll
+  for (int i = 0; i < ((!NORM && XB == 2) ? 0 : NV); ++i) {
 #pragma unroll
     for (int j = 0; j < E; ++j) {
       float v = rx[i].get(j, a.x_bf16);
@@ -211,14 +250,18 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
     top = __reduce_max_sync(0xffffffffu, lane < T / 32 ? red_t[lane] : 0u);
   }
   const float rstd = NORM ? rsqrtf(ss / static_cast<float>(a.d) + a.eps) : 1.0f;
-  float inv = 1.0f;
+  float inv = 1.0f, unit = 1.0f, m = 1.0f;
   if (a.y_dtype == HB_DTYPE_E4M3) {
     const float amax = __uint_as_float(top) * rstd;
     const bool finite = amax <= 3.402823466e38f;   // (false for NaN too)
-    const float m = fmaxf(amax, 7.888609052210118e-31f);   // 2^-100: 448 / m is finite
+    m = fmaxf(amax, 7.888609052210118e-31f);   // 2^-100: 448 / m is finite
     inv = finite ? 448.0f / m : __int_as_float(0x7fffffff);
-    if (tid == 0) a.scale[r] = finite ? m / 448.0f : __int_as_float(0x7fffffff);
+    unit = finite ? m * (1.0f / 448.0f) : __int_as_float(0x7fffffff);   // (within 2^-23; bit for bit PyTorch's m / 448)
+    if (tid == 0) a.scale[r] = unit;
   }
+  // Rows as they came have values next to borders of codes far more often than chance has it (few bits, ratios of small
+  // numbers): their codes are the quotient's by the scale that is handed out.  A norm's values carry errors of their own.
+  const Quotient over_unit(unit, m);
   if constexpr (!NORM && E == 8) {
     if (a.turned) {
       // codes where the boundaries of their own row lie, then out in 8-byte accesses
@@ -229,9 +272,13 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int at = first(i);
+        float v[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = rx[i].get(j, a.x_bf16);
+        over_unit(v);
 #pragma unroll
         for (int j = 0; j < E; ++j)
-          if (at + j >= 0 && at + j < a.d) mine[y_lead + at + j] = __nv_cvt_float_to_fp8(rx[i].get(j, a.x_bf16) * inv, __NV_SATFINITE, __NV_E4M3);
+          if (at + j >= 0 && at + j < a.d) mine[y_lead + at + j] = __nv_cvt_float_to_fp8(v[j], __NV_SATFINITE, __NV_E4M3);
       }
       if constexpr (T == 32) __syncwarp();
       else __syncthreads();
@@ -258,11 +305,12 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
       if constexpr (NORM) {
         v[j] = s[i][j] * rstd;
         if (has_gain) v[j] *= rg[i].get(j, 1);
+        v[j] *= inv;
       } else {
         v[j] = rx[i].get(j, a.x_bf16);     // (kept as loaded: half the registers)
       }
-      v[j] *= inv;
     }
+    if constexpr (!NORM) over_unit(v);
     put<E>(y, at, a.y_dtype, whole(at), a.d, v);
   }
 }
