@@ -737,6 +737,8 @@ int hb_mixed_step_lora(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, c
 int hb_mixed_step8(hb_ctx* c, const hb_batch_desc* d, const hb_weights8* w, hb_kv* kv, hb_pool* pool, float* out_logits,
                    float* out_emb, void* stream) {
   if (!c || !w || !w->layers || !kv || !kv->e4m3) return HB_ERR_BAD_ARG;
+  // the rows that go to codes: a block holds one whole
+  if (c->cfg.d_ffn > HB_NORM_MAX_D || static_cast<int64_t>(c->cfg.n_heads) * c->cfg.head_dim > HB_NORM_MAX_D) return HB_ERR_TOO_LARGE;
   for (int l = 0; l < c->cfg.n_layers; ++l) {
     const hb_layer_weights8& x = w->layers[l];
     if (!x.attn_norm || !x.ffn_norm || !x.wqkv || !x.wo || !x.w_gate_up || !x.w_down || !x.wqkv_scale || !x.wo_scale || !x.gate_up_scale || !x.down_scale)

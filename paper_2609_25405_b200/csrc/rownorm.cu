@@ -391,6 +391,7 @@ int wrong_device(const hb_ctx* c) {
 }  // namespace
 
 int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl) {
+  if (n.d > HB_NORM_MAX_D) return HB_ERR_TOO_LARGE;   // (no variant covers more)
   RowArgs a = {};
   a.x = n.x; a.res = n.residual; a.sum = n.sum_out; a.gain = static_cast<const __nv_bfloat16*>(n.gain); a.y = n.y; a.scale = n.y_scale;
   a.status = c->status;
@@ -411,6 +412,7 @@ int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl) {
 
 int hb_launch_quant_rows(hb_ctx* c, const void* x, int x_dtype, int64_t x_stride, int n_src, const int32_t* index, int n_rows, int d,
                          void* codes, int64_t codes_stride, float* scale, cudaStream_t s, bool pdl) {
+  if (d > HB_NORM_MAX_D) return HB_ERR_TOO_LARGE;
   RowArgs a = {};
   a.x = x; a.y = codes; a.scale = scale; a.index = index; a.status = c->status;
   a.x_stride = x_stride; a.y_stride = codes_stride;
