@@ -697,7 +697,9 @@ HB_API int hb_linear_grouped(hb_ctx* ctx, const hb_linear_args* args, const int3
  * hb_quant_rows, hb_linear down onto the residual stream.  Embedding, gains, LM head, pooling and outputs are hb_mixed_step's.
  * Every projection weight is E4M3 codes, row-major [out, in] in hb_layer_weights' row order, 16-byte aligned, with a float
  * scale per row (hb_quant_rows of the model's rows gives both).  No adapters.  d_ffn and n_heads * head_dim are at most
- * HB_NORM_MAX_D (HB_ERR_TOO_LARGE).  A row's projections depend on the number of rows of the step in their last bits (hb_linear), unlike hb_mixed_step's.  HB_STATUS_F16_RANGE is raised by the first norm only. */
+ * HB_NORM_MAX_D (HB_ERR_TOO_LARGE).  A row's projections depend on the number of rows of the step in their last bits (hb_linear), unlike hb_mixed_step's.
+ * HB_STATUS_F16_RANGE: a normed row held a NaN or an infinity, or a row of the attention's output or of the SwiGLU held a NaN or reached
+ * +-65504, where hb_linear saturates. */
 typedef struct {
   const void *attn_norm, *ffn_norm;                 /* bf16 [d_model] */
   const void *wqkv, *wo, *w_gate_up, *w_down;       /* E4M3 codes */

@@ -27,9 +27,9 @@ __device__ __forceinline__ void f16x4_to_float4(uint2 raw, float4& o) {
 }
 
 // x[t,:] = E[tok[t],:] (kept in fp32 as the residual stream); h[t,:] = fp16(rmsnorm(x) * gain).
-// GATHER = false: x is read instead.  NV = 16-byte vectors a thread holds: 4 covers d_model <= 4096 in
+// GATHER = false: x is read instead; NORM = false: x alone is wanted.  NV = 16-byte vectors a thread holds: 4 covers d_model <= 4096 in
 // few enough registers for eight blocks per SM (more rows in flight per SM), 8 covers d_model <= 8192.
-template <bool GATHER, int NV>
+template <bool GATHER, int NV, bool NORM = true>
 __global__ void __launch_bounds__(NORM_THREADS, NV == 4 ? 8 : 4)
 norm_kernel(const int32_t* __restrict__ tok, const __nv_bfloat16* __restrict__ E,
             const __nv_bfloat16* __restrict__ gain, float* __restrict__ x, __half* __restrict__ h,
@@ -56,6 +56,7 @@ norm_kernel(const int32_t* __restrict__ tok, const __nv_bfloat16* __restrict__ E
       ss += buf[i].x * buf[i].x + buf[i].y * buf[i].y + buf[i].z * buf[i].z + buf[i].w * buf[i].w;
     }
   }
+  if constexpr (!NORM) return;
   const float tot = block_sum(ss, red);
   const float rstd = rsqrtf(tot / static_cast<float>(d) + eps);
   __half* hrow = h + static_cast<size_t>(t) * d;
@@ -220,6 +221,12 @@ int hb_launch_embed_norm(hb_ctx* c, const void* tok_emb, const void* gain, cudaS
   return hb_launch_kernel(norm_kernel<true, MAX_VEC>, c->dd.T, NORM_THREADS, 0, s, c->pdl, c->dd.tok,
                           static_cast<const __nv_bfloat16*>(tok_emb), static_cast<const __nv_bfloat16*>(gain), c->x,
                           c->h, c->cfg.d_model, c->cfg.rms_eps, c->status);
+}
+
+int hb_launch_embed(hb_ctx* c, const void* tok_emb, cudaStream_t s) {
+  return hb_launch_kernel(norm_kernel<true, MAX_VEC, false>, c->dd.T, NORM_THREADS, 0, s, c->pdl, c->dd.tok,
+                          static_cast<const __nv_bfloat16*>(tok_emb), nullptr, c->x, nullptr, c->cfg.d_model,
+                          c->cfg.rms_eps, c->status);
 }
 
 int hb_launch_rmsnorm(hb_ctx* c, const void* gain, cudaStream_t s) {

@@ -222,6 +222,7 @@ inline int hb_launch_kernel(void (*kern)(KArgs...), unsigned grid, unsigned bloc
 // ---- elementwise / attention launchers ---------------------------------------
 struct hb_ctx;
 int hb_launch_embed_norm(hb_ctx* c, const void* tok_emb, const void* gain, cudaStream_t s);
+int hb_launch_embed(hb_ctx* c, const void* tok_emb, cudaStream_t s);   // the fp32 rows alone
 int hb_launch_rmsnorm(hb_ctx* c, const void* gain, cudaStream_t s);
 // The step's attention launch of one layer.  `which` selects the item lists it serves (both in the
 // step itself; one at a time when launches are timed per class).
@@ -238,9 +239,10 @@ int hb_launch_pool_chunk(hb_ctx* c, const float* x, const void* gain, int n_rows
 int hb_launch_bf16_to_f16(const void* src, void* dst, size_t n, cudaStream_t s);
 
 // dense operators (rownorm.cu, linear.cu); arguments already checked
-int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl);
+// report: raise HB_DEV_F16_RANGE for a row whose scale is NaN, or an fp16 row that reached the largest half
+int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl, bool report = false);
 int hb_launch_quant_rows(hb_ctx* c, const void* x, int x_dtype, int64_t x_stride, int n_src, const int32_t* index, int n_rows, int d,
-                         void* codes, int64_t codes_stride, float* scale, cudaStream_t s, bool pdl);
+                         void* codes, int64_t codes_stride, float* scale, cudaStream_t s, bool pdl, bool report = false);
 // group_start NULL: one group of all rows
 int hb_launch_linear(hb_ctx* c, const hb_linear_args& l, const int32_t* group_start, int n_groups, int64_t w_group_stride,
                      cudaStream_t s, bool pdl);

@@ -698,11 +698,11 @@ struct Layer8 {
     n.x = c->x; n.gain = gain; n.y = c->h; n.y_scale = row_scale();
     n.x_stride = n.y_stride = n.d = c->cfg.d_model;
     n.x_dtype = HB_DTYPE_F32; n.y_dtype = HB_DTYPE_E4M3; n.n_rows = T; n.eps = c->cfg.rms_eps;
-    return hb_launch_norm(c, n, s, c->pdl);
+    return hb_launch_norm(c, n, s, c->pdl, true);
   }
   // fp16 rows to codes in place: a row's codes take the first half of its bytes, and whoever writes them has read all of them
   int codes(__half* x, int d) const {
-    return hb_launch_quant_rows(c, x, HB_DTYPE_F16, d, T, nullptr, T, d, x, 2 * d, row_scale(), s, c->pdl);
+    return hb_launch_quant_rows(c, x, HB_DTYPE_F16, d, T, nullptr, T, d, x, 2 * d, row_scale(), s, c->pdl, true);
   }
   int project(const void* a, int a_stride, const void* weight, const float* scale, void* out, int n, int k, int dtype, bool residual, bool swiglu) const {
     hb_linear_args l = {};
@@ -1023,7 +1023,7 @@ int mixed_step(hb_ctx* c, const hb_batch_desc* d, const hb_weights* w, const hb_
   };
   for (int l = 0; layers8 && l < cfg.n_layers; ++l) {
     const Layer8 y{c, layers8[l], T, s};
-    if (l == 0) HB_TRY(HB_CLASS_NORM_ROPE, hb_launch_embed_norm(c, w->tok_emb, y.w.attn_norm, s));   // (its fp16 rows are not used)
+    if (l == 0) HB_TRY(HB_CLASS_NORM_ROPE, hb_launch_embed(c, w->tok_emb, s));
     HB_TRY(HB_CLASS_NORM_ROPE, y.norm(y.w.attn_norm));
     HB_TRY(HB_CLASS_GEMM, y.project(c->h, cfg.d_model, y.w.wqkv, y.w.wqkv_scale, c->act, n_qkv, cfg.d_model, HB_DTYPE_F16, false, false));
     if ((rc = attend8(l)) != HB_OK) return rc;

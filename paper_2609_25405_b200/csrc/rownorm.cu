@@ -34,6 +34,7 @@ struct RowArgs {
   int32_t lead0, lead_step;   // elements between a 16-byte boundary and the start of row r: (lead0 + r lead_step) mod 8
   int32_t turned, y_lead0, y_lead_step;   // hb_quant_rows: codes not aligned as x is go through `turned` bytes of shared memory per row
   float eps;
+  int32_t report;             // of a row's scale and, where rows are fp16, of a largest magnitude that may be a saturated one
 };
 
 __device__ __forceinline__ float from16(uint32_t bits16, int bf16) {
@@ -257,7 +258,10 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
     m = fmaxf(amax, 7.888609052210118e-31f);   // 2^-100: 448 / m is finite
     inv = finite ? 448.0f / m : __int_as_float(0x7fffffff);
     unit = finite ? m * (1.0f / 448.0f) : __int_as_float(0x7fffffff);   // (within 2^-23; bit for bit PyTorch's m / 448)
-    if (tid == 0) a.scale[r] = unit;
+    if (tid == 0) {
+      a.scale[r] = unit;
+      if (a.report && (!finite || (!NORM && XB == 2 && !a.x_bf16 && amax >= 65504.0f))) atomicOr(a.status, HB_DEV_F16_RANGE);
+    }
   }
   // Rows as they came have values next to borders of codes far more often than chance has it (few bits, ratios of small
   // numbers): their codes are the quotient's by the scale that is handed out.  A norm's values carry errors of their own.
@@ -390,11 +394,11 @@ int wrong_device(const hb_ctx* c) {
 
 }  // namespace
 
-int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl) {
+int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl, bool report) {
   if (n.d > HB_NORM_MAX_D) return HB_ERR_TOO_LARGE;   // (no variant covers more)
   RowArgs a = {};
   a.x = n.x; a.res = n.residual; a.sum = n.sum_out; a.gain = static_cast<const __nv_bfloat16*>(n.gain); a.y = n.y; a.scale = n.y_scale;
-  a.status = c->status;
+  a.status = c->status; a.report = report;
   a.x_stride = n.x_stride; a.res_stride = n.residual_stride; a.sum_stride = n.sum_stride; a.y_stride = n.y_stride;
   a.n_rows = n.n_rows; a.n_src = n.n_rows; a.d = n.d;
   a.x_bf16 = n.x_dtype == HB_DTYPE_BF16; a.res_bf16 = n.residual_dtype == HB_DTYPE_BF16; a.y_dtype = n.y_dtype; a.eps = n.eps;
@@ -411,10 +415,10 @@ int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl) {
 }
 
 int hb_launch_quant_rows(hb_ctx* c, const void* x, int x_dtype, int64_t x_stride, int n_src, const int32_t* index, int n_rows, int d,
-                         void* codes, int64_t codes_stride, float* scale, cudaStream_t s, bool pdl) {
+                         void* codes, int64_t codes_stride, float* scale, cudaStream_t s, bool pdl, bool report) {
   if (d > HB_NORM_MAX_D) return HB_ERR_TOO_LARGE;
   RowArgs a = {};
-  a.x = x; a.y = codes; a.scale = scale; a.index = index; a.status = c->status;
+  a.x = x; a.y = codes; a.scale = scale; a.index = index; a.status = c->status; a.report = report;
   a.x_stride = x_stride; a.y_stride = codes_stride;
   a.n_rows = n_rows; a.n_src = n_src; a.d = d;
   a.x_bf16 = x_dtype == HB_DTYPE_BF16; a.y_dtype = HB_DTYPE_E4M3;
