@@ -691,6 +691,11 @@ HB_API int hb_linear(hb_ctx* ctx, const hb_linear_args* args, void* stream);
 HB_API int hb_linear_grouped(hb_ctx* ctx, const hb_linear_args* args, const int32_t* group_start, int32_t n_groups,
                              int64_t w_group_stride, void* stream);
 
+/* Which kernel the two calls take for these sizes and types on a device of num_sms SMs (n_groups 0: hb_linear); host only, pointers and
+ * strides are not looked at.  out[0]: rows of A per tile (8 and 16: the kernel for few rows; 256: a pair of CTAs), out[1]: blocks of 16
+ * features of such a small tile, or the CTAs that share a tile's K, out[2]: how the sums leave (0 plain, 1 in segments, 2 sixteen warps). */
+HB_API int hb_linear_variant(const hb_linear_args* args, int32_t n_groups, int32_t num_sms, int32_t out[3]);
+
 /* The step with 8-bit projection weights: hb_mixed_step over an 8-bit cache (hb_kv8_create) whose four projections per layer
  * run on E4M3 operands.  Per layer: hb_norm to codes, hb_linear QKV, append and attention over the 8-bit cache,
  * hb_quant_rows of the attention's output, hb_linear O onto the residual stream, hb_norm, hb_linear gate/up with SwiGLU,

@@ -133,6 +133,7 @@ _sig = {
     "hb_quant_rows": [_P, _P, C.c_int32, C.c_int64, C.c_int32, _P, C.c_int32, C.c_int32, _P, C.c_int64, _P, _P],
     "hb_linear": [_P, C.POINTER(LinearArgs), _P],
     "hb_linear_grouped": [_P, C.POINTER(LinearArgs), _P, C.c_int32, C.c_int64, _P],
+    "hb_linear_variant": [C.POINTER(LinearArgs), C.c_int32, C.c_int32, C.POINTER(C.c_int32)],
     "hb_rope_table": [C.c_int32, C.c_int32, C.c_double, C.POINTER(RopeScaling), _P, _P],
     "hb_pool_arena_bytes": [C.POINTER(ModelCfg), C.c_int32, C.POINTER(C.c_size_t)],
     "hb_pool_create": [C.POINTER(ModelCfg), _P, C.c_size_t, C.c_int32, C.POINTER(_P)],

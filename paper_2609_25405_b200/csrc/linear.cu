@@ -1061,13 +1061,19 @@ int launch_narrow(const hb_linear_args& l, const LinArgs& a, int64_t w_group_str
   return l.ab_dtype == HB_DTYPE_E4M3 ? launch_narrow_as<MT, NT, true>(l, a, w_group_stride, s, pdl) : launch_narrow_as<MT, NT, false>(l, a, w_group_stride, s, pdl);
 }
 
+// How the epilogue of an unshared tile of `tokens` works.
+int mode_of(const hb_linear_args& l, int k_blocks, int tokens) {
+  if (l.c_dtype == HB_DTYPE_F32 && k_blocks > SEG_BLOCKS) return LONG;
+  return tokens >= 128 && k_blocks <= (tokens == 128 ? 8 : 12) ? SHORT : PLAIN;
+}
+
 template <int CG, int BT, bool SPLIT>
 int launch(const hb_linear_args& l, const LinArgs& a, int splits, int num_sms, int64_t w_group_stride, cudaStream_t s, bool pdl) {
   if constexpr (!SPLIT) {
-    if (l.c_dtype == HB_DTYPE_F32 && a.k_blocks > SEG_BLOCKS)
-      return launch_as<CG, BT, SPLIT, LONG>(l, a, splits, num_sms, w_group_stride, s, pdl);
+    const int mode = mode_of(l, a.k_blocks, BT);
+    if (mode == LONG) return launch_as<CG, BT, SPLIT, LONG>(l, a, splits, num_sms, w_group_stride, s, pdl);
     if constexpr (BT >= 128) {
-      if (a.k_blocks <= (BT == 128 ? 8 : 12)) return launch_as<CG, BT, SPLIT, SHORT>(l, a, splits, num_sms, w_group_stride, s, pdl);
+      if (mode == SHORT) return launch_as<CG, BT, SPLIT, SHORT>(l, a, splits, num_sms, w_group_stride, s, pdl);
     }
   }
   return launch_as<CG, BT, SPLIT, PLAIN>(l, a, splits, num_sms, w_group_stride, s, pdl);
@@ -1077,13 +1083,14 @@ int launch(const hb_linear_args& l, const LinArgs& a, int splits, int num_sms, i
 // blocks of a narrow tile, or the CTAs that share a tile's K.
 struct Variant {
   int tokens, share;
-  float us;
+  float us, own;   // the estimate, and the same without what every variant waits for, the weights
 };
 
 // Each variant's time in microseconds from the sizes, with what was measured on a B200 (n, k from 300 x 1000 to 28672 x 4096 and
 // 1024 x 8192, 1 to 4000 rows, both operand widths); the least wins.  What it decides, both sides measured (us):
 //   8 rows, 2048 x 2048, 16 bits    narrow 5.2, one CTA per tile 11.3, four per tile 9.5
-//   8 rows, 28672 x 4096, 8 bits    narrow 31.6, one CTA per tile 25.9
+//   8 rows, 28672 x 4096, 8 bits    narrow 31.6, one CTA per tile 26.6, pairs 28.0
+//   64 rows, 28672 x 4096, 8 bits   one CTA per tile of 64 27.3, pairs 28.7
 //   64 rows, 1024 x 8192, 16 bits   narrow 19.0, one CTA per tile 31.1, eight per tile 13.7
 //   300 rows, 4096 x 4096, 16 bits  128 tokens 21.4, pairs 27.5
 //   2000 rows, 4096 x 4096, 16 bits 128 tokens 69.2, pairs 52.4
@@ -1098,9 +1105,9 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
     return t > groups ? t : static_cast<float>(groups);
   };
   auto ceil_div = [](float x, float y) { return ceilf(x / y); };
-  Variant best = {256, 1, 1e30f};
-  auto offer = [&](int tokens, int share, float us) {
-    if (us < best.us) best = {tokens, share, us};
+  Variant best = {256, 1, 1e30f, 1e30f};
+  auto offer = [&](int tokens, int share, float us, float own) {
+    if (us < best.us || (us == best.us && own < best.own)) best = {tokens, share, us, own};
   };
   if (rows <= 64.0f) {
     for (int nt = 1; nt <= 2; ++nt)
@@ -1109,7 +1116,8 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
         const float rounds = ceil_div(k_bytes, 512.0f * (mt * nt == 1 ? 8 : mt * nt == 2 ? 4 : 2));   // of loads that wait for each other
         const float waves = ceil_div(blocks, 2 * sms);
         const float latency = rounds * (mt * nt == 1 ? 2.1f : mt * nt == 2 ? 1.7f : 1.4f), bytes = blocks * (16 * mt + 8 * nt) * k_bytes / 6e6f;
-        offer(8 * nt, mt, 1.0f + waves * (1.0f + mt) + (waves * latency > bytes ? waves * latency : bytes));
+        const float us = 1.0f + waves * (1.0f + mt) + (waves * latency > bytes ? waves * latency : bytes);
+        offer(8 * nt, mt, us, us);
       }
   }
   const bool f8 = l.ab_dtype == HB_DTYPE_E4M3;
@@ -1121,20 +1129,35 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
     const float out_us = bt == 32 ? 0.9f : bt == 64 ? 1.25f : bt == 128 ? 2.0f : 4.0f;      // a tile's epilogue
     const float main_us = k_blocks * block_us, waves = ceil_div(tiles, bt == 256 ? sms / 2 : sms);
     const float us = 4.2f + main_us + out_us + (waves - 1.0f) * (main_us > out_us ? main_us : out_us);
-    offer(bt, 1, us > weight_us + 4.5f ? us : weight_us + 4.5f + 0.1f * us);   // (both bound by the weights: the one with more to spare)
+    offer(bt, 1, us > weight_us + 4.5f ? us : weight_us + 4.5f, us);   // (of several bound by the weights: the one with most to spare)
     if (bt == 256) break;
     for (int s = 4; s <= 8 && s <= k_blocks; s *= 2) {                         // (two never paid)
       const float ctas = tiles * s, held = rows < bt ? rows : static_cast<float>(bt);
       if (ctas > 2 * sms) break;                                               // all at once, two per SM, or not at all
       const float share_us = ceil_div(k_blocks, s) * (ctas > sms ? 0.45f : 0.3f);
       const float split_us = share_us > weight_us ? share_us : weight_us;
-      offer(bt, s, 7.8f + split_us + held / 128.0f * (2.0f + 12.0f / s));
+      const float split = 7.8f + split_us + held / 128.0f * (2.0f + 12.0f / s);
+      offer(bt, s, split, split);
     }
   }
   return best;
 }
 
 }  // namespace
+
+namespace {
+int k_blocks_of(const hb_linear_args& l) { return static_cast<int>((static_cast<int64_t>(l.k) * elem_bytes(l.ab_dtype) + BKB - 1) / BKB); }
+}  // namespace
+
+extern "C" int hb_linear_variant(const hb_linear_args* l, int32_t n_groups, int32_t num_sms, int32_t* out) {
+  if (!l || !out || l->m < 1 || l->n < 1 || l->k < 1 || n_groups < 0 || num_sms < 1) return HB_ERR_BAD_ARG;
+  const int k_blocks = k_blocks_of(*l);
+  const Variant v = pick_variant(*l, n_groups > 0 ? n_groups : 1, k_blocks, n_groups > 0, num_sms);
+  out[0] = v.tokens;
+  out[1] = v.share;
+  out[2] = v.tokens >= 32 && v.share == 1 ? mode_of(*l, k_blocks, v.tokens) : PLAIN;
+  return HB_OK;
+}
 
 int hb_launch_linear(hb_ctx* c, const hb_linear_args& l, const int32_t* group_start, int n_groups, int64_t w_group_stride,
                      cudaStream_t s, bool pdl) {
@@ -1143,7 +1166,7 @@ int hb_launch_linear(hb_ctx* c, const hb_linear_args& l, const int32_t* group_st
   a.start = group_start;
   a.n_groups = n_groups;
   a.status = c->status;
-  a.k_blocks = static_cast<int>((static_cast<int64_t>(l.k) * elem_bytes(l.ab_dtype) + BKB - 1) / BKB);
+  a.k_blocks = k_blocks_of(l);
   const int sms = c->num_sms;
   const Variant v = pick_variant(l, n_groups, a.k_blocks, group_start != nullptr, sms);
   switch (v.tokens * 10 + v.share) {
