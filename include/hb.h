@@ -664,7 +664,8 @@ enum { HB_ACT_NONE = 0, HB_ACT_RELU = 1, HB_ACT_SILU = 2, HB_ACT_GELU = 3, HB_AC
  *   a_scale   float [m] or NULL, w_scale float [n] or NULL (any ab_dtype), bias float [n] or NULL
  *   residual  [m, columns of C] F32, F16 or BF16, or NULL; may be c itself where type and stride are c's
  *   c         [m, n or n / 2] F32, F16 or BF16; may not overlap a or w
- * Device pointers.  Products are summed in fp32 on the tensor cores, everything after them in fp32, rounded once.
+ * Device pointers.  Products are summed in fp32 on the tensor cores, everything after them in fp32, rounded once.  The tensor cores
+ * truncate: terms of one sign lose up to 2.5e-5 of their sum before it is added in registers that round (1e-4 with 16 bits out).
  * The order of a sum depends on the sizes (m among them), never on values or timing: equal calls give equal bits. */
 typedef struct {
   const void* a;

@@ -38,7 +38,13 @@ namespace {
 constexpr int BF = 128;                 // features per CTA
 constexpr int BKB = 128;                // bytes of K per k-block
 constexpr int MAX_STAGES = 12;
-constexpr int SEG_BLOCKS = 10;          // k-blocks summed in tensor memory between additions in registers (fp32 outputs)
+// The tensor cores cut what falls off the end of a running sum, always towards zero: per instruction (32 bytes of K) 2^-26 of the sum where
+// its terms have both signs, up to 2^-23.4 where they have one (fp16; K = 4096 in four shares: 5.9e-6).  So a chain of additions in one
+// accumulator is bounded: where a whole tile is one CTA's, sums leave tensor memory after SEG_BLOCKS k-blocks and are added in registers
+// (fp32 outputs; 16-bit outputs from KEEP_16 k-blocks on, where the loss comes near a fifth of their half step, 9e-5); tiles whose K is
+// shared and the kernel for few rows are taken only where a share is at most KEEP_32 or KEEP_16 k-blocks (2.4e-5 at worst, or 9e-5).
+constexpr int SEG_BLOCKS = 10;
+constexpr int KEEP_32 = 64, KEEP_16 = 256;
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;   // 2 s
 
 struct LinArgs {
@@ -382,9 +388,7 @@ __device__ __forceinline__ void issue_block(uint32_t d, uint64_t wdesc, uint64_t
 }
 
 // How a persistent CTA's epilogue works.  PLAIN: 8 warps, a residual ahead.  LONG: tensor memory holds a tile's sums for SEG_BLOCKS k-blocks
-// at a time, and registers (of 16 warps) add them up.  The tensor cores cut what falls off the end of a sum, 2^-26 of it per
-// instruction on average and always towards zero (fp16, K = 14336: 1.7e-5 in all); additions in registers round.  For fp32
-// outputs; with 16 bits out the loss is far below the rounding.  SHORT: 16 warps, for products of so few k-blocks that the
+// at a time, and registers (of 16 warps) add them up, where additions round.  SHORT: 16 warps, for products of so few k-blocks that the
 // results bound them (4096 x 4096 x 64 fp16: 17.9 us, with 8 warps 19.8; at K = 4096 the 8 warps' larger ring wins by 2 %).
 enum { PLAIN = 0, LONG = 1, SHORT = 2 };
 
@@ -1063,7 +1067,7 @@ int launch_narrow(const hb_linear_args& l, const LinArgs& a, int64_t w_group_str
 
 // How the epilogue of an unshared tile of `tokens` works.
 int mode_of(const hb_linear_args& l, int k_blocks, int tokens) {
-  if (l.c_dtype == HB_DTYPE_F32 && k_blocks > SEG_BLOCKS) return LONG;
+  if (k_blocks > (l.c_dtype == HB_DTYPE_F32 ? SEG_BLOCKS : KEEP_16)) return LONG;
   return tokens >= 128 && k_blocks <= (tokens == 128 ? 8 : 12) ? SHORT : PLAIN;
 }
 
@@ -1109,7 +1113,8 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
   auto offer = [&](int tokens, int share, float us, float own) {
     if (us < best.us || (us == best.us && own < best.own)) best = {tokens, share, us, own};
   };
-  if (rows <= 64.0f) {
+  const int keep = l.c_dtype == HB_DTYPE_F32 ? KEEP_32 : KEEP_16;            // k-blocks in one accumulator, at most
+  if (rows <= 64.0f && k_blocks <= NARROW_WARPS * keep) {
     for (int nt = 1; nt <= 2; ++nt)
       for (int mt = 1; mt <= 2; ++mt) {
         const float blocks = ceil_div(l.n, 16 * mt) * token_tiles(8 * nt);
@@ -1134,6 +1139,7 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
     for (int s = 4; s <= 8 && s <= k_blocks; s *= 2) {                         // (two never paid)
       const float ctas = tiles * s, held = rows < bt ? rows : static_cast<float>(bt);
       if (ctas > 2 * sms) break;                                               // all at once, two per SM, or not at all
+      if (ceil_div(k_blocks, s) > keep) continue;
       const float share_us = ceil_div(k_blocks, s) * (ctas > sms ? 0.45f : 0.3f);
       const float split_us = share_us > weight_us ? share_us : weight_us;
       const float split = 7.8f + split_us + held / 128.0f * (2.0f + 12.0f / s);

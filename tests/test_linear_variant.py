@@ -32,6 +32,20 @@ def test_more_weights_do_not_move_the_choice_back():
         assert 256 not in took
 
 
+def test_chains_of_additions_are_bounded():
+    """fp32 outputs: at most 64 k-blocks (128 bytes of K) in one accumulator, or sums that leave in segments; 16 bits out: 256."""
+    for ab, size in ((F16, 2), (E4M3, 1)):
+        for c_t, most in ((F32, 64), (F16, 256)):
+            for m in (1, 8, 16, 33, 64, 100, 200, 500, 3000):
+                for n in (16, 150, 1024, 5000):
+                    for k in (64, 5000, 14336, 32768, 65537, 1 << 18, 1 << 22):
+                        for groups in (0, 4):
+                            tokens, share, mode = variant(m, n, k, ab, c_t, groups)
+                            blocks = (k * size + 127) // 128
+                            blocks = -(-blocks // 8) if tokens <= 16 else 10 if mode == 1 else -(-blocks // share)
+                            assert blocks <= most, (m, n, k, ab, c_t, groups)
+
+
 def test_refusals():
     out = (C.c_int32 * 3)()
     good = dict(m=4, n=32, k=64, ab_dtype=F16, c_dtype=F32)
