@@ -99,7 +99,7 @@ __device__ __forceinline__ void activate(float (&z)[SIZE], int act) {
 
 // A warp's block of results, 32 features (one per lane) of 32 tokens, on its way out.  It is laid down in shared memory as
 // [token][column] (16 columns where gated pairs became one) and leaves by one TMA copy; where rows of C or of the residual do not start on
-// 16-byte boundaries, or the block holds rows of another group, the warp copies it with the widest accesses that the alignment
+// 16-byte boundaries, or the block holds rows of another group or the end of rows off such a boundary, the warp copies it with the widest accesses that the alignment
 // allows.  The residual comes in the same way, into the same place, ahead of the sums.
 struct Block {
   const LinArgs& a;
@@ -248,7 +248,8 @@ struct Block {
     scale(z, factor, bias, as, scales);
     if (a.l.gated) compute<16>(z, arrived);
     else compute<32>(z, arrived);
-    if (a.c_tma && whole()) {
+    // (a copy's rows end on 16-byte boundaries, whatever the tensor map says of their length: it would write behind C's)
+    if (a.c_tma && whole() && (cols() >= width() || cols() * (a.l.c_dtype == HB_DTYPE_F32 ? 4 : 2) % 16 == 0)) {
       fence_async_smem();
       __syncwarp();
       if (issuer) tma_store_2d(map, buf, col0, row0);
