@@ -304,7 +304,8 @@ class DeviceWeights8:
         self.struct.layers = C.cast(self.layers, C.POINTER(LayerWeights8))
         self.codes = [{} for _ in range(n_layers)]   # per layer: name -> (codes, scale)
         self._device = device
-        self._ctx = Context(ModelCfg(1, 64, 1, 1, 64, 64, 64, 16, 64, 1e4, 1e-5), 1, 1, 1)   # quantises the rows
+        with torch.cuda.device(device):
+            self._ctx = Context(ModelCfg(1, 64, 1, 1, 64, 64, 64, 16, 64, 1e4, 1e-5), 1, 1, 1)   # quantises the rows, on that device
 
     def _keep(self, t):
         self.tensors.append(t)
@@ -314,14 +315,19 @@ class DeviceWeights8:
         """Quantises the rows of w [out, in] (bf16, fp16 or fp32 on the device)."""
         codes = torch.empty(w.shape, dtype=torch.float8_e4m3fn, device=w.device)
         scale = torch.empty(w.shape[0], dtype=torch.float32, device=w.device)
-        self._ctx.quant_rows(w, codes, scale)
+        with torch.cuda.device(self._device):
+            self._ctx.quant_rows(w, codes, scale)
         self.codes[layer][name] = (codes, scale)
         setattr(self.layers[layer], name, self._keep(codes))
         setattr(self.layers[layer], scale_name, self._keep(scale))
 
+    def _packed_head(self, lm_head):
+        with torch.cuda.device(self._device):
+            return pack_f16_(lm_head)
+
     def _rest(self, tok_emb, final_norm, lm_head):
         self.struct.tok_emb, self.struct.final_norm, self.struct.lm_head = (self._keep(t) for t in (tok_emb, final_norm, lm_head))
-        torch.cuda.synchronize()      # the rows' sources go when the caller's do
+        torch.cuda.synchronize(self._device)      # the rows' sources go when the caller's do
         self._ctx.close()
         return self
 
@@ -340,7 +346,7 @@ class DeviceWeights8:
             for name, scale, a in (("wqkv", "wqkv_scale", qkv), ("wo", "wo_scale", w["wo"]), ("w_gate_up", "gate_up_scale", gu),
                                    ("w_down", "down_scale", w["wd"])):
                 self._set(l, name, scale, up(a))
-        return self._rest(up(W.tok_emb), up(W.final_norm), pack_f16_(up(W.lm_head)))
+        return self._rest(up(W.tok_emb), up(W.final_norm), self._packed_head(up(W.lm_head)))
 
     @classmethod
     def random_on_device(cls, shape, seed=0, std=0.02, device="cuda"):
@@ -355,7 +361,7 @@ class DeviceWeights8:
             for name, scale, r, c in (("wqkv", "wqkv_scale", shape.n_qkv, shape.d), ("wo", "wo_scale", shape.d, shape.Hq * shape.Dh),
                                       ("w_gate_up", "gate_up_scale", 2 * shape.F, shape.d), ("w_down", "down_scale", shape.d, shape.F)):
                 self._set(l, name, scale, rnd(r, c))
-        return self._rest(rnd(shape.V, shape.d), ones(), pack_f16_(rnd(shape.V, shape.d)))
+        return self._rest(rnd(shape.V, shape.d), ones(), self._packed_head(rnd(shape.V, shape.d)))
 
 
 def _pad64(n):
