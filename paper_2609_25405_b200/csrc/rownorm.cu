@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
 
 template <int XB, int RB, int T, int NV, int E, bool NORM>
 int launch(const RowArgs& a, cudaStream_t s, bool pdl) {
-  const unsigned grid = T == 32 ? (a.n_rows + 7) / 8 : a.n_rows;
+  const unsigned rows = static_cast<unsigned>(a.n_rows), grid = T == 32 ? (rows + 7) / 8 : rows;   // (n_rows may be the largest int)
   return hb_launch_kernel(row_kernel<XB, RB, T, NV, E, NORM>, grid, T == 32 ? 256 : T, (T == 32 ? 8 : 1) * a.turned, s, pdl, a);
 }
 
