@@ -687,6 +687,8 @@ def _matrix(t, device_index, name):
     if len(shape) == 2 and t.get_device() == device_index and t.dtype in _DTYPES:
         rows, cols = shape
         stride, unit = t.stride()
+        if rows > 0x7fffffff or cols > 0x7fffffff:
+            raise ValueError(f"{name}: at most 2^31 - 1 rows and columns")
         if unit == 1 or cols == 1 or rows == 0 or cols == 0:
             return t.data_ptr(), rows, cols, (stride if rows > 1 else (cols + 15) // 16 * 16), _DTYPES[t.dtype]   # (one row: any stride)
     raise ValueError(f"{name}: an fp32, fp16, bf16 or e4m3 matrix with unit column stride on cuda:{device_index}")
@@ -920,6 +922,8 @@ class Context:
             raise ValueError(f"w: fp16, bf16 or e4m3 [groups, n, k] on cuda:{dev}")
         groups, n, k = shape
         step, ws, unit = w.stride()
+        if max(shape) > 0x7fffffff:
+            raise ValueError("w: at most 2^31 - 1 groups, rows and columns")
         if unit != 1 and k > 1:
             raise ValueError("w: unit stride along k")
         if n == 1:
