@@ -617,8 +617,9 @@ HB_API int hb_logprobs(hb_ctx* ctx, const void* logits, int32_t dtype, int32_t n
  * bias, activation and residual in its epilogue, with one weight (hb_linear) or one per run of rows
  * (hb_linear_grouped).  Types are HB_DTYPE_*; strides are in elements and may exceed the row length.
  * E4M3 rows carry one fp32 scale each, max(their largest magnitude, 2^-100) / 448 (by the rounded
- * reciprocal): code c stands for c * scale.  A row that holds a NaN or an infinity has scale NaN and NaN codes.  fp16 outputs saturate at +-65504 (NaN stays NaN).  Nothing is allocated, and no call keeps
- * anything for the next: calls of one context may run at the same time on different streams. */
+ * reciprocal): code c stands for c * scale.  A row that holds a NaN or an infinity has scale NaN and NaN codes.  fp16 outputs
+ * saturate at +-65504 (NaN stays NaN).  Nothing is allocated, and no call keeps anything for the next: calls of one context may run at
+ * the same time on different streams. */
 
 /* y = s / sqrt(mean(s^2) + eps) * gain with s = x (+ residual), one pass over the row.  Device pointers.
  *   x         [n_rows, d] F32, F16 or BF16
@@ -628,8 +629,9 @@ HB_API int hb_logprobs(hb_ctx* ctx, const void* logits, int32_t dtype, int32_t n
  *   gain      bf16 [d], or NULL = ones
  *   y         [n_rows, d] F32, F16, BF16 or E4M3; may be x itself where type and stride are x's
  *   y_scale   float [n_rows], E4M3 only (NULL otherwise)
- * Pointers aligned to their type, 1 <= d <= HB_NORM_MAX_D; rows that start on 16-byte boundaries (8 for
- * E4M3) with d a multiple of 8 are read and written in wide accesses.  Statistics in fp32. */
+ * Pointers aligned to their type, 1 <= d <= HB_NORM_MAX_D; rows are read and written in wide accesses where the arrays' rows
+ * lie alike against 16-byte boundaries (8 for E4M3) and the gain starts on one, whatever d.  Statistics in fp32; a row whose
+ * squares sum beyond fp32 norms to zero, as the formula does in fp32. */
 #define HB_NORM_MAX_D 32768
 typedef struct {
   const void* x;
@@ -653,7 +655,8 @@ HB_API int hb_norm(hb_ctx* ctx, const hb_norm_args* args, void* stream);
 HB_API int hb_quant_rows(hb_ctx* ctx, const void* x, int32_t x_dtype, int64_t x_stride, int32_t n_src, const int32_t* index,
                          int32_t n_rows, int32_t d, void* codes, int64_t codes_stride, float* scale, void* stream);
 
-/* Activations of hb_linear; GELU is x Phi(x), GELU_TANH its form with tanh. */
+/* Activations of hb_linear; GELU is x Phi(x), GELU_TANH its form with tanh.  Their errors are 2^-20 of |x| at most, not of the result:
+ * where GELU is small beside x (x = -5: 3e-7 x), some of its own bits are lost. */
 enum { HB_ACT_NONE = 0, HB_ACT_RELU = 1, HB_ACT_SILU = 2, HB_ACT_GELU = 3, HB_ACT_GELU_TANH = 4 };
 
 /* C = act(z) + residual,  z[i, j] = a_scale[i] * w_scale[j] * sum_k a[i, k] * w[j, k] + bias[j]
@@ -687,7 +690,8 @@ HB_API int hb_linear(hb_ctx* ctx, const hb_linear_args* args, void* stream);
  * [n_groups, n].  Groups are an expert's rows, or the requests that share an adapter; a group may be empty.
  * group_start: device int32 [n_groups + 1], not decreasing, in 0 .. m; read on the device only, so a captured call sees what
  * it holds when it is replayed.  Rows before the first and behind the last group are left as they are.  A group that
- * starts below an earlier bound, ends before it starts or leaves 0 .. m is skipped and raises HB_STATUS_GROUP_INDEX.  n_groups <= HB_LINEAR_MAX_GROUPS. */
+ * starts below an earlier bound, ends before it starts or leaves 0 .. m is skipped and raises HB_STATUS_GROUP_INDEX.
+ * n_groups <= HB_LINEAR_MAX_GROUPS. */
 #define HB_LINEAR_MAX_GROUPS 512
 HB_API int hb_linear_grouped(hb_ctx* ctx, const hb_linear_args* args, const int32_t* group_start, int32_t n_groups,
                              int64_t w_group_stride, void* stream);
@@ -703,9 +707,10 @@ HB_API int hb_linear_variant(const hb_linear_args* args, int32_t n_groups, int32
  * hb_quant_rows, hb_linear down onto the residual stream.  Embedding, gains, LM head, pooling and outputs are hb_mixed_step's.
  * Every projection weight is E4M3 codes, row-major [out, in] in hb_layer_weights' row order, 16-byte aligned, with a float
  * scale per row (hb_quant_rows of the model's rows gives both).  No adapters.  d_ffn and n_heads * head_dim are at most
- * HB_NORM_MAX_D (HB_ERR_TOO_LARGE).  A row's projections depend on the number of rows of the step in their last bits (hb_linear), unlike hb_mixed_step's.
- * HB_STATUS_F16_RANGE: a normed row held a NaN or an infinity, or a row of the attention's output or of the SwiGLU held a NaN or reached
- * +-65504, where hb_linear saturates. */
+ * HB_NORM_MAX_D (HB_ERR_TOO_LARGE).  A row's projections depend on the number of rows of the step in their last bits
+ * (hb_linear), unlike hb_mixed_step's.
+ * HB_STATUS_F16_RANGE: a normed row held a NaN or an infinity, or a row of the attention's output or of the SwiGLU held a
+ * NaN or reached +-65504, where hb_linear saturates. */
 typedef struct {
   const void *attn_norm, *ffn_norm;                 /* bf16 [d_model] */
   const void *wqkv, *wo, *w_gate_up, *w_down;       /* E4M3 codes */

@@ -239,6 +239,8 @@ int hb_launch_pool_chunk(hb_ctx* c, const float* x, const void* gain, int n_rows
 int hb_launch_bf16_to_f16(const void* src, void* dst, size_t n, cudaStream_t s);
 
 // dense operators (rownorm.cu, linear.cu); arguments already checked
+inline int hb_elem_bytes(int dtype) { return dtype == HB_DTYPE_F32 ? 4 : dtype == HB_DTYPE_E4M3 ? 1 : 2; }
+inline bool hb_float_type(int dtype) { return dtype == HB_DTYPE_F32 || dtype == HB_DTYPE_F16 || dtype == HB_DTYPE_BF16; }
 // report: raise HB_DEV_F16_RANGE for a row whose scale is NaN, or an fp16 row that reached the largest half
 int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl, bool report = false);
 int hb_launch_quant_rows(hb_ctx* c, const void* x, int x_dtype, int64_t x_stride, int n_src, const int32_t* index, int n_rows, int d,
@@ -315,3 +317,10 @@ struct hb_ctx {
   int32_t last_launches;
   bool pdl;   // the next launch may overlap the tail of the previous kernel (set inside a step)
 };
+
+// launches go to the current device: HB_ERR_BAD_ARG where that is not the context's
+inline int hb_wrong_device(const hb_ctx* c) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return HB_ERR_CUDA;
+  return dev == c->device ? HB_OK : HB_ERR_BAD_ARG;
+}

@@ -704,7 +704,8 @@ struct Layer8 {
   int codes(__half* x, int d) const {
     return hb_launch_quant_rows(c, x, HB_DTYPE_F16, d, T, nullptr, T, d, x, 2 * d, row_scale(), s, c->pdl, true);
   }
-  int project(const void* a, int a_stride, const void* weight, const float* scale, void* out, int n, int k, int dtype, bool residual, bool swiglu) const {
+  int project(const void* a, int a_stride, const void* weight, const float* scale, void* out, int n, int k, int dtype, bool residual,
+              bool swiglu) const {
     hb_linear_args l = {};
     l.a = a; l.a_stride = a_stride; l.a_scale = row_scale();
     l.w = weight; l.w_stride = k; l.w_scale = scale;
@@ -741,11 +742,12 @@ int hb_mixed_step8(hb_ctx* c, const hb_batch_desc* d, const hb_weights8* w, hb_k
   if (c->cfg.d_ffn > HB_NORM_MAX_D || static_cast<int64_t>(c->cfg.n_heads) * c->cfg.head_dim > HB_NORM_MAX_D) return HB_ERR_TOO_LARGE;
   for (int l = 0; l < c->cfg.n_layers; ++l) {
     const hb_layer_weights8& x = w->layers[l];
-    if (!x.attn_norm || !x.ffn_norm || !x.wqkv || !x.wo || !x.w_gate_up || !x.w_down || !x.wqkv_scale || !x.wo_scale || !x.gate_up_scale || !x.down_scale)
-      return HB_ERR_BAD_ARG;
-    if (misaligned(x.attn_norm, 8) || misaligned(x.ffn_norm, 8) || misaligned(x.wqkv, 16) || misaligned(x.wo, 16) || misaligned(x.w_gate_up, 16) ||
-        misaligned(x.w_down, 16) || misaligned(x.wqkv_scale, 4) || misaligned(x.wo_scale, 4) || misaligned(x.gate_up_scale, 4) || misaligned(x.down_scale, 4))
-      return HB_ERR_BAD_ARG;
+    for (const void* gain : {x.attn_norm, x.ffn_norm})
+      if (!gain || misaligned(gain, 8)) return HB_ERR_BAD_ARG;
+    for (const void* codes : {x.wqkv, x.wo, x.w_gate_up, x.w_down})
+      if (!codes || misaligned(codes, 16)) return HB_ERR_BAD_ARG;
+    for (const float* scale : {x.wqkv_scale, x.wo_scale, x.gate_up_scale, x.down_scale})
+      if (!scale || misaligned(scale, 4)) return HB_ERR_BAD_ARG;
   }
   const hb_weights rest = {w->tok_emb, nullptr, w->final_norm, w->lm_head};
   return mixed_step(c, d, &rest, nullptr, w->layers, kv, pool, out_logits, out_emb, stream);

@@ -62,7 +62,7 @@ struct LinArgs {
 };
 
 // x Phi(x), with the complement of erf after Abramowitz and Stegun 7.1.26: erfc(u) = (a1 t + .. + a5 t^5) exp(-u^2), t = 1 / (1 + p u),
-// u >= 0, off by at most 1.5e-7, which is 2^-23 |x| here.  Half the instructions of erff, and no branches.
+// u >= 0, off by at most 1.5e-7, which is 2^-23 |x| here (of GELU itself 0.2 % at x = -5 and 2 % at -10).  Half the instructions of erff, and no branches.
 __device__ __forceinline__ float gelu(float x) {
   const float u = fabsf(x) * 0.70710678f, t = __fdividef(1.0f, fmaf(0.3275911f, u, 1.0f));
   float p = fmaf(1.061405429f, t, -1.453152027f);
@@ -98,9 +98,9 @@ __device__ __forceinline__ void activate(float (&z)[SIZE], int act) {
 }
 
 // A warp's block of results, 32 features (one per lane) of 32 tokens, on its way out.  It is laid down in shared memory as
-// [token][column] (16 columns where gated pairs became one) and leaves by one TMA copy; where rows of C or of the residual do not start on
-// 16-byte boundaries, or the block holds rows of another group or the end of rows off such a boundary, the warp copies it with the widest accesses that the alignment
-// allows.  The residual comes in the same way, into the same place, ahead of the sums.
+// [token][column] (16 columns where gated pairs became one) and leaves by one TMA copy; where rows of C or of the residual do not
+// start on 16-byte boundaries, or the block holds rows of another group or the end of rows off such a boundary, the warp copies it
+// with the widest accesses that the alignment allows.  The residual comes in the same way, into the same place, ahead of the sums.
 struct Block {
   const LinArgs& a;
   char* mem;            // this block in shared memory, and its address there
@@ -126,7 +126,8 @@ struct Block {
     const int token = lane >> shift, at = (lane - (token << shift)) * V, step = 32 >> shift;   // first token, byte in its row, tokens per pass
     if (at >= cols() * size) return;        // (V divides the row's bytes)
     char* g = base + (row0 + token) * stride_bytes + col0 * size + at;
-    using Vec = typename std::conditional<V == 16, uint4, typename std::conditional<V == 8, uint2, typename std::conditional<V == 4, uint32_t, unsigned short>::type>::type>::type;
+    using Small = typename std::conditional<V == 4, uint32_t, unsigned short>::type;
+    using Vec = typename std::conditional<V == 16, uint4, typename std::conditional<V == 8, uint2, Small>::type>::type;
     int s = lane * V;
     stride_bytes *= step;
 #pragma unroll 8
@@ -403,7 +404,8 @@ struct Shape {
   static constexpr int EPI_WARPS = BT / 8 < MOST ? BT / 8 : MOST;
   static constexpr int PARTS = EPI_WARPS / 4;
   static constexpr int THREADS = 64 + EPI_WARPS * 32;
-  static constexpr int BAR_BYTES = 8 * (2 * MAX_STAGES + 4 + 2 * 16) + 8 + 24;   // full, empty, tfull, tempty, one per buffer; two words; to a multiple of 32
+  // full, empty, tfull, tempty, one per buffer; two words; to a multiple of 32
+  static constexpr int BAR_BYTES = 8 * (2 * MAX_STAGES + 4 + 2 * 16) + 8 + 24;
   static constexpr int SCALE_BYTES = EPI_WARPS * 32 * 4;
   static constexpr int STAGE_BYTES = W_BYTES + TOKENS * BKB;
 };
@@ -455,7 +457,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
   int* g_hi = g_lo + a.n_groups;
   int* g_pre = g_hi + a.n_groups;   // [n_groups + 1]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr uint32_t tmem_cols = SPLIT ? BT : 2 * BT;   // one accumulator where a CTA has one tile   // one accumulator where a CTA has one tile
+  constexpr uint32_t tmem_cols = SPLIT ? BT : 2 * BT;   // one accumulator where a CTA has one tile
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
@@ -639,7 +641,8 @@ linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ 
       const int64_t f_at = static_cast<int64_t>(t.group) * a.l.n + f0 + lane;
       const float factor = mine && a.l.w_scale ? a.l.w_scale[f_at] : 1.0f, bias = mine && a.l.bias ? a.l.bias[f_at] : 0.0f;
       auto block_at = [&](const Tile& tile, int feature, int c, int i) {
-        return Block{a, buf_mem + i * a.buf_bytes, bufs + static_cast<uint32_t>(i * a.buf_bytes), issuer, lane, tile.row0 + c, min(32, tile.rows - c), a.l.gated ? feature >> 1 : feature};
+        return Block{a, buf_mem + i * a.buf_bytes, bufs + static_cast<uint32_t>(i * a.buf_bytes), issuer, lane, tile.row0 + c,
+                     min(32, tile.rows - c), a.l.gated ? feature >> 1 : feature};
       };
       auto block_of = [&](int c, int i) { return block_at(t, f0, c, i); };
       // buffer i can be written: what was copied out of it has been read
@@ -951,37 +954,25 @@ __global__ void __launch_bounds__(NARROW_WARPS * 32, 2) linear_narrow_kernel(con
   finish_tokens<MINE>(l, z, as, factor, bias, t.row0 + token0, STEP, count, feature, lane);
 }
 
-int elem_bytes(int dtype) { return dtype == HB_DTYPE_F32 ? 4 : dtype == HB_DTYPE_E4M3 ? 1 : 2; }
-bool float_type(int dtype) { return dtype == HB_DTYPE_F32 || dtype == HB_DTYPE_F16 || dtype == HB_DTYPE_BF16; }
 bool on(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
 int check(const hb_ctx* c, const hb_linear_args* l) {
   if (!c || !l || l->m < 0 || l->n < 1 || l->k < 1) return HB_ERR_BAD_ARG;
   if (l->ab_dtype != HB_DTYPE_F16 && l->ab_dtype != HB_DTYPE_BF16 && l->ab_dtype != HB_DTYPE_E4M3) return HB_ERR_BAD_ARG;
-  if (!float_type(l->c_dtype) || (l->residual && !float_type(l->residual_dtype))) return HB_ERR_BAD_ARG;
+  if (!hb_float_type(l->c_dtype) || (l->residual && !hb_float_type(l->residual_dtype))) return HB_ERR_BAD_ARG;
   if (l->act < HB_ACT_NONE || l->act > HB_ACT_GELU_TANH || (l->gated != 0 && l->gated != 1) || (l->gated && l->n % 2)) return HB_ERR_BAD_ARG;
   if (l->m > (1 << 26) || l->n > (1 << 26) || l->k > (1 << 26)) return HB_ERR_TOO_LARGE;
-  const int ab = elem_bytes(l->ab_dtype), cols = l->gated ? l->n / 2 : l->n;
+  const int ab = hb_elem_bytes(l->ab_dtype), cols = l->gated ? l->n / 2 : l->n;
   if (l->a_stride < l->k || l->w_stride < l->k || l->c_stride < cols || (l->residual && l->residual_stride < cols)) return HB_ERR_BAD_ARG;
   if (l->a_stride > (1ll << 36) || l->w_stride > (1ll << 36) || l->c_stride > (1ll << 36) || (l->residual && l->residual_stride > (1ll << 36)))
     return HB_ERR_TOO_LARGE;
   if (!on(l->a, 16) || !on(l->w, 16) || (l->a_stride * ab) % 16 || (l->w_stride * ab) % 16) return HB_ERR_BAD_ARG;
-  if (!on(l->c, elem_bytes(l->c_dtype)) || (l->residual && !on(l->residual, elem_bytes(l->residual_dtype))) || !on(l->a_scale, 4) ||
+  if (!on(l->c, hb_elem_bytes(l->c_dtype)) || (l->residual && !on(l->residual, hb_elem_bytes(l->residual_dtype))) || !on(l->a_scale, 4) ||
       !on(l->w_scale, 4) || !on(l->bias, 4))
     return HB_ERR_BAD_ARG;
   if (l->m > 0 && (!l->a || !l->w || !l->c)) return HB_ERR_BAD_ARG;
   return HB_OK;
 }
-
-int wrong_device(const hb_ctx* c) {
-  int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess) return HB_ERR_CUDA;
-  return dev == c->device ? HB_OK : HB_ERR_BAD_ARG;   // launches go to the current device
-}
-
-}  // namespace
-
-namespace {
 
 // Largest access (up to 16 bytes) that fits the rows' alignment and length.
 int row_vector(const void* p, int64_t stride, int size, int cols) {
@@ -993,7 +984,7 @@ int row_vector(const void* p, int64_t stride, int size, int cols) {
 template <int CG, int BT, bool SPLIT, int MODE>
 int launch_as(const hb_linear_args& l, LinArgs a, int splits, int num_sms, int64_t w_group_stride, cudaStream_t s, bool pdl) {
   using S = Shape<CG, BT, MODE>;
-  const int ab = elem_bytes(l.ab_dtype);
+  const int ab = hb_elem_bytes(l.ab_dtype);
   CUtensorMap tw, ta;
   const uint64_t k_bytes = static_cast<uint64_t>(l.k) * ab;
   int rc = hb_tmap_bytes(&tw, l.w, k_bytes, l.n, a.n_groups, l.w_stride * ab, (a.start ? w_group_stride : l.w_stride) * ab, BKB, BF);
@@ -1008,7 +999,8 @@ int launch_as(const hb_linear_args& l, LinArgs a, int splits, int num_sms, int64
   if (items > (1ll << 30)) return HB_ERR_TOO_LARGE;
   const int table = 4 * (3 * a.n_groups + 1);
   // results: TMA copies where rows start on 16-byte boundaries
-  const int width = l.gated ? 16 : 32, cols = l.gated ? l.n / 2 : l.n, cs = elem_bytes(l.c_dtype), rs = l.residual ? elem_bytes(l.residual_dtype) : 0;
+  const int width = l.gated ? 16 : 32, cols = l.gated ? l.n / 2 : l.n;
+  const int cs = hb_elem_bytes(l.c_dtype), rs = l.residual ? hb_elem_bytes(l.residual_dtype) : 0;
   CUtensorMap tc = ta, tr = ta;
   if constexpr (!SPLIT) {
     a.c_vec = row_vector(l.c, l.c_stride, cs, cols);
@@ -1063,8 +1055,11 @@ int launch_narrow_as(const hb_linear_args& l, LinArgs a, int64_t w_group_stride,
 }
 template <int MT, int NT>
 int launch_narrow(const hb_linear_args& l, const LinArgs& a, int64_t w_group_stride, cudaStream_t s, bool pdl) {
-  return l.ab_dtype == HB_DTYPE_E4M3 ? launch_narrow_as<MT, NT, true>(l, a, w_group_stride, s, pdl) : launch_narrow_as<MT, NT, false>(l, a, w_group_stride, s, pdl);
+  return l.ab_dtype == HB_DTYPE_E4M3 ? launch_narrow_as<MT, NT, true>(l, a, w_group_stride, s, pdl)
+                                     : launch_narrow_as<MT, NT, false>(l, a, w_group_stride, s, pdl);
 }
+
+int k_blocks_of(const hb_linear_args& l) { return static_cast<int>((static_cast<int64_t>(l.k) * hb_elem_bytes(l.ab_dtype) + BKB - 1) / BKB); }
 
 // How the epilogue of an unshared tile of `tokens` works.
 int mode_of(const hb_linear_args& l, int k_blocks, int tokens) {
@@ -1152,10 +1147,6 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
 
 }  // namespace
 
-namespace {
-int k_blocks_of(const hb_linear_args& l) { return static_cast<int>((static_cast<int64_t>(l.k) * elem_bytes(l.ab_dtype) + BKB - 1) / BKB); }
-}  // namespace
-
 extern "C" int hb_linear_variant(const hb_linear_args* l, int32_t n_groups, int32_t num_sms, int32_t* out) {
   if (!l || !out || l->m < 1 || l->n < 1 || l->k < 1 || n_groups < 0 || num_sms < 1) return HB_ERR_BAD_ARG;
   const int k_blocks = k_blocks_of(*l);
@@ -1195,7 +1186,7 @@ int hb_launch_linear(hb_ctx* c, const hb_linear_args& l, const int32_t* group_st
 extern "C" int hb_linear(hb_ctx* c, const hb_linear_args* l, void* stream) {
   int rc = check(c, l);
   if (rc != HB_OK || l->m == 0) return rc;
-  if ((rc = wrong_device(c)) != HB_OK) return rc;
+  if ((rc = hb_wrong_device(c)) != HB_OK) return rc;
   return hb_launch_linear(c, *l, nullptr, 1, 0, static_cast<cudaStream_t>(stream), false);
 }
 
@@ -1205,9 +1196,9 @@ extern "C" int hb_linear_grouped(hb_ctx* c, const hb_linear_args* l, const int32
   if (rc != HB_OK) return rc;
   if (n_groups < 1 || !on(group_start, 4) || w_group_stride < static_cast<int64_t>(l->n - 1) * l->w_stride + l->k) return HB_ERR_BAD_ARG;
   if (n_groups > HB_LINEAR_MAX_GROUPS || w_group_stride > (1ll << 36)) return HB_ERR_TOO_LARGE;
-  if ((w_group_stride * elem_bytes(l->ab_dtype)) % 16) return HB_ERR_BAD_ARG;
+  if ((w_group_stride * hb_elem_bytes(l->ab_dtype)) % 16) return HB_ERR_BAD_ARG;
   if (l->m == 0) return HB_OK;
   if (!group_start) return HB_ERR_BAD_ARG;
-  if ((rc = wrong_device(c)) != HB_OK) return rc;
+  if ((rc = hb_wrong_device(c)) != HB_OK) return rc;
   return hb_launch_linear(c, *l, group_start, n_groups, w_group_stride, static_cast<cudaStream_t>(stream), false);
 }

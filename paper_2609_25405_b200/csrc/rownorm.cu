@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) row_kernel(const RowArgs a)
   if constexpr (!NORM && E == 8) {
     if (a.turned) {
       // codes where the boundaries of their own row lie, then out in 8-byte accesses
-      extern __shared__ unsigned char codes[];
+      extern __shared__ __align__(16) unsigned char codes[];
       const int y_lead = static_cast<int>((a.y_lead0 + r * a.y_lead_step) & 7);
       unsigned char* mine = codes + threadIdx.x / T * a.turned;
       unsigned char* y = static_cast<unsigned char*>(a.y) + r * a.y_stride;
@@ -372,24 +372,17 @@ bool aligned_alike(std::initializer_list<Rows> arrays, RowArgs* a) {
   const int64_t lead = reinterpret_cast<uintptr_t>(ref->p) / ref->size % 8, step = ref->stride % 8;
   for (const Rows& x : arrays) {
     const int64_t unit = x.size == 4 ? 4 : 8;
-    if (x.p && ((reinterpret_cast<uintptr_t>(x.p) / x.size) % unit != static_cast<uint64_t>(lead % unit) || x.stride % unit != step % unit)) return false;
+    if (!x.p) continue;
+    if ((reinterpret_cast<uintptr_t>(x.p) / x.size) % unit != static_cast<uint64_t>(lead % unit) || x.stride % unit != step % unit) return false;
   }
   a->lead0 = static_cast<int32_t>(lead);
   a->lead_step = static_cast<int32_t>(step);
   return true;
 }
 
-int elem_bytes(int dtype) { return dtype == HB_DTYPE_F32 ? 4 : dtype == HB_DTYPE_E4M3 ? 1 : 2; }
-bool float_type(int dtype) { return dtype == HB_DTYPE_F32 || dtype == HB_DTYPE_F16 || dtype == HB_DTYPE_BF16; }
 // Every row starts on a boundary of `bytes`.
 bool rows_on(const void* p, int64_t stride, int size, int bytes) {
   return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (stride * size) % bytes == 0;
-}
-
-int wrong_device(const hb_ctx* c) {
-  int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess) return HB_ERR_CUDA;
-  return dev == c->device ? HB_OK : HB_ERR_BAD_ARG;   // launches go to the current device
 }
 
 }  // namespace
@@ -402,9 +395,10 @@ int hb_launch_norm(hb_ctx* c, const hb_norm_args& n, cudaStream_t s, bool pdl, b
   a.x_stride = n.x_stride; a.res_stride = n.residual_stride; a.sum_stride = n.sum_stride; a.y_stride = n.y_stride;
   a.n_rows = n.n_rows; a.n_src = n.n_rows; a.d = n.d;
   a.x_bf16 = n.x_dtype == HB_DTYPE_BF16; a.res_bf16 = n.residual_dtype == HB_DTYPE_BF16; a.y_dtype = n.y_dtype; a.eps = n.eps;
-  const int xb = elem_bytes(n.x_dtype), rb = n.residual ? elem_bytes(n.residual_dtype) : 0, yb = elem_bytes(n.y_dtype);
+  const int xb = hb_elem_bytes(n.x_dtype), rb = n.residual ? hb_elem_bytes(n.residual_dtype) : 0, yb = hb_elem_bytes(n.y_dtype);
   const bool wide = rows_on(n.gain, 0, 2, 16) &&
-                    aligned_alike({{n.x, n.x_stride, xb}, {n.residual, n.residual_stride, rb ? rb : 1}, {n.sum_out, n.sum_stride, rb ? rb : 1}, {n.y, n.y_stride, yb}}, &a);
+                    aligned_alike({{n.x, n.x_stride, xb}, {n.residual, n.residual_stride, rb ? rb : 1},
+                                   {n.sum_out, n.sum_stride, rb ? rb : 1}, {n.y, n.y_stride, yb}}, &a);
   const bool many = n.n_rows >= 2 * c->num_sms;
   if (xb == 4) {
     if (rb == 0) return launch_size<4, 0, true>(a, wide, many, s, pdl);
@@ -422,7 +416,7 @@ int hb_launch_quant_rows(hb_ctx* c, const void* x, int x_dtype, int64_t x_stride
   a.x_stride = x_stride; a.y_stride = codes_stride;
   a.n_rows = n_rows; a.n_src = n_src; a.d = d;
   a.x_bf16 = x_dtype == HB_DTYPE_BF16; a.y_dtype = HB_DTYPE_E4M3;
-  const int xb = elem_bytes(x_dtype);
+  const int xb = hb_elem_bytes(x_dtype);
   if (!aligned_alike({{x, x_stride, xb}, {codes, codes_stride, 1}}, &a) || (index && a.lead_step)) {   // (an index breaks the step)
     a.y_lead0 = static_cast<int32_t>(reinterpret_cast<uintptr_t>(codes) % 8);
     a.y_lead_step = static_cast<int32_t>(codes_stride % 8);
@@ -437,31 +431,31 @@ int hb_launch_quant_rows(hb_ctx* c, const void* x, int x_dtype, int64_t x_stride
 
 extern "C" int hb_norm(hb_ctx* c, const hb_norm_args* n, void* stream) {
   if (!c || !n || n->n_rows < 0 || n->d < 1 || !(n->eps >= 0.0f)) return HB_ERR_BAD_ARG;
-  if (!float_type(n->x_dtype) || (n->residual && !float_type(n->residual_dtype)) || (!float_type(n->y_dtype) && n->y_dtype != HB_DTYPE_E4M3))
+  if (!hb_float_type(n->x_dtype) || (n->residual && !hb_float_type(n->residual_dtype)) || (!hb_float_type(n->y_dtype) && n->y_dtype != HB_DTYPE_E4M3))
     return HB_ERR_BAD_ARG;
   if ((n->sum_out && !n->residual) || (n->y_scale && n->y_dtype != HB_DTYPE_E4M3)) return HB_ERR_BAD_ARG;
   if (n->d > HB_NORM_MAX_D) return HB_ERR_TOO_LARGE;
   if (n->x_stride < n->d || n->y_stride < n->d || (n->residual && n->residual_stride < n->d) || (n->sum_out && n->sum_stride < n->d))
     return HB_ERR_BAD_ARG;
-  const int xb = elem_bytes(n->x_dtype), rb = n->residual ? elem_bytes(n->residual_dtype) : 1;
+  const int xb = hb_elem_bytes(n->x_dtype), rb = n->residual ? hb_elem_bytes(n->residual_dtype) : 1;
   if (!rows_on(n->x, 0, 1, xb) || !rows_on(n->residual, 0, 1, rb) || !rows_on(n->sum_out, 0, 1, rb) || !rows_on(n->gain, 0, 1, 2) ||
-      !rows_on(n->y, 0, 1, elem_bytes(n->y_dtype)) || !rows_on(n->y_scale, 0, 1, 4))
+      !rows_on(n->y, 0, 1, hb_elem_bytes(n->y_dtype)) || !rows_on(n->y_scale, 0, 1, 4))
     return HB_ERR_BAD_ARG;
   if (n->n_rows == 0) return HB_OK;
   if (!n->x || !n->y || (n->y_dtype == HB_DTYPE_E4M3 && !n->y_scale)) return HB_ERR_BAD_ARG;
-  const int rc = wrong_device(c);
+  const int rc = hb_wrong_device(c);
   return rc != HB_OK ? rc : hb_launch_norm(c, *n, static_cast<cudaStream_t>(stream), false);
 }
 
 extern "C" int hb_quant_rows(hb_ctx* c, const void* x, int32_t x_dtype, int64_t x_stride, int32_t n_src, const int32_t* index,
                              int32_t n_rows, int32_t d, void* codes, int64_t codes_stride, float* scale, void* stream) {
-  if (!c || n_rows < 0 || n_src < 0 || d < 1 || !float_type(x_dtype) || (!index && n_src < n_rows)) return HB_ERR_BAD_ARG;
+  if (!c || n_rows < 0 || n_src < 0 || d < 1 || !hb_float_type(x_dtype) || (!index && n_src < n_rows)) return HB_ERR_BAD_ARG;
   if (d > HB_NORM_MAX_D) return HB_ERR_TOO_LARGE;
   if (x_stride < d || codes_stride < d) return HB_ERR_BAD_ARG;
-  if (!rows_on(x, 0, 1, elem_bytes(x_dtype)) || !rows_on(index, 0, 1, 4) || !rows_on(scale, 0, 1, 4)) return HB_ERR_BAD_ARG;
+  if (!rows_on(x, 0, 1, hb_elem_bytes(x_dtype)) || !rows_on(index, 0, 1, 4) || !rows_on(scale, 0, 1, 4)) return HB_ERR_BAD_ARG;
   if (n_rows == 0) return HB_OK;
   if ((!x && n_src > 0) || !codes || !scale) return HB_ERR_BAD_ARG;
-  const int rc = wrong_device(c);
+  const int rc = hb_wrong_device(c);
   return rc != HB_OK ? rc
                      : hb_launch_quant_rows(c, x, x_dtype, x_stride, n_src, index, n_rows, d, codes, codes_stride, scale,
                                             static_cast<cudaStream_t>(stream), false);
