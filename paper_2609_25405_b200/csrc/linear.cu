@@ -20,8 +20,8 @@
 //   few rows   linear_narrow_kernel below
 //
 // What bounds it (one B200, 148 SMs): 4096 x 28672 x 4096 e4m3 with SwiGLU 310 - 330 us, 2.9 - 3.1 PFLOP/s, the tensor pipe and the
-// power limit (a k-block takes 512 cycles of it); 64 rows of 28672 x 4096 e4m3 25 us and eight such weights 150 us, HBM
-// (4.7 and 6.2 TB/s); 2048^3 fp16 onto fp32 26 us, one wave of tiles: filling, 32 k-blocks, and an epilogue that nothing hides.
+// power limit (a k-block takes 512 cycles of it); 64 rows of 28672 x 4096 e4m3 26 us and eight such weights 151 us, HBM
+// (4.6 and 6.2 TB/s); 2048^3 fp16 onto fp32 28 us, one wave of tiles: filling, 32 k-blocks, and an epilogue that nothing hides.
 //
 // Groups: every CTA reads the bounds, drops those that are no good and numbers the token tiles of the others; a weight is a
 // three-dimensional tensor map, so that a tile never sees the next group's rows.
@@ -390,7 +390,8 @@ __device__ __forceinline__ void issue_block(uint32_t d, uint64_t wdesc, uint64_t
 }
 
 // How a persistent CTA's epilogue works.  PLAIN: 8 warps, a residual ahead.  LONG: tensor memory holds a tile's sums for SEG_BLOCKS k-blocks
-// at a time, and registers (of 16 warps) add them up, where additions round.  SHORT: 16 warps, for products of so few k-blocks that the
+// at a time, and registers (of 16 warps) add them up, where additions round; the pairs' 18 warps leave 96 registers a thread, of which two
+// blocks of sums take 64, and some 300 bytes a thread are spilled.  SHORT: 16 warps, for products of so few k-blocks that the
 // results bound them (4096 x 4096 x 64 fp16: 17.9 us, with 8 warps 19.8; at K = 4096 the 8 warps' larger ring wins by 2 %).
 enum { PLAIN = 0, LONG = 1, SHORT = 2 };
 

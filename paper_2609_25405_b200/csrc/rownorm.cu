@@ -7,9 +7,12 @@
 // written once.  The largest |y| is rstd * max |s * gain| with rstd > 0, so the sum of squares and the maximum
 // come out of ONE reduction and an 8-bit output needs no second pass over the row.
 //
-// Measured (one B200; 6.46 TB/s is a copy): 4096 rows of 4096, fp16 + fp32 to fp32 and codes, 29 us = 6.4 TB/s; 4096 rows of 14336
+// Measured (one B200; 6.46 TB/s is a copy): 4096 rows of 4096, fp16 + fp32 to fp32 and codes, 29 - 31 us = 6.0 - 6.4 TB/s; 2048 rows of
+// 16384, 20000 and 32768 the same way 70, 104 and 143 us = 5.3, 4.3 and 5.2 TB/s (with a residual more than 16384 columns spill 70 to
+// 270 bytes a thread); 4096 rows of 14336
 // fp16 to codes 35.6 us = 4.9 TB/s (gathered 38.9); rows off every boundary (4096 of 4097, fp16 + fp32 to codes) 52 us = 3.5 TB/s, with
-// one element per access 88.
+// one element per access 88; arrays aligned differently, which have to: 2048 rows of 8000 55 us, of 20000 389 us = 1.2 TB/s
+// (32 values a thread and array, 80 to 860 bytes of them spilled).
 #include <cuda_fp8.h>
 
 #include <initializer_list>
