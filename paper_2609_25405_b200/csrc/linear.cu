@@ -1150,6 +1150,7 @@ Variant pick_variant(const hb_linear_args& l, int n_groups, int k_blocks, bool g
 
 extern "C" int hb_linear_variant(const hb_linear_args* l, int32_t n_groups, int32_t num_sms, int32_t* out) {
   if (!l || !out || l->m < 1 || l->n < 1 || l->k < 1 || n_groups < 0 || num_sms < 1) return HB_ERR_BAD_ARG;
+  if (l->m > (1 << 26) || l->n > (1 << 26) || l->k > (1 << 26) || n_groups > HB_LINEAR_MAX_GROUPS) return HB_ERR_TOO_LARGE;
   const int k_blocks = k_blocks_of(*l);
   const Variant v = pick_variant(*l, n_groups > 0 ? n_groups : 1, k_blocks, n_groups > 0, num_sms);
   out[0] = v.tokens;

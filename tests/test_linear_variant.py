@@ -51,7 +51,10 @@ def test_refusals():
     good = dict(m=4, n=32, k=64, ab_dtype=F16, c_dtype=F32)
     for kw in (dict(m=0), dict(n=0), dict(k=0)):
         assert B.lib.hb_linear_variant(C.byref(B.LinearArgs(**dict(good, **kw))), 0, 148, out) == -1
+    for kw in (dict(m=(1 << 26) + 1), dict(n=2 ** 31 - 1), dict(k=2 ** 31 - 1)):
+        assert B.lib.hb_linear_variant(C.byref(B.LinearArgs(**dict(good, **kw))), 0, 148, out) == -5
     a = B.LinearArgs(**good)
+    assert B.lib.hb_linear_variant(C.byref(a), B.LINEAR_MAX_GROUPS + 1, 148, out) == -5
     assert B.lib.hb_linear_variant(None, 0, 148, out) == -1 and B.lib.hb_linear_variant(C.byref(a), 0, 148, None) == -1
     assert B.lib.hb_linear_variant(C.byref(a), -1, 148, out) == -1 and B.lib.hb_linear_variant(C.byref(a), 0, 0, out) == -1
     assert B.lib.hb_linear_variant(C.byref(a), 0, 148, out) == 0
